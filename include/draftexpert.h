@@ -589,6 +589,106 @@ int de_distill_signals(const de_model* m, int T, const int32_t* tokens, float ta
                        float* m_star, float* router_kl, float* logit_kl, float* token_ce,
                        void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- Token scores and distillation from a teacher's top logits ----
+ *
+ * Row operators over a vocabulary, with gradients: what a program that scores
+ * tokens, stores a teacher's most likely tokens or trains a drafter on them
+ * (Eq. 8 against a short list, Eq. 9) computes from logits.
+ *
+ * Shared by the calls below
+ *   - logits [rows, ld], first V of each row, DE_F32 or DE_BF16 (dtype), aligned
+ *     to their element only; ld >= V.  Row offsets are 64-bit.
+ *   - p = softmax(logits / tau), 1e-30 <= tau <= 1e30.  Sums, logarithms and
+ *     gradients are taken in 32 bits or more whatever the logits' type; a bf16
+ *     gradient is rounded once, to nearest.
+ *   - 1 <= rows <= 2^20, 1 <= V <= 2^30, and rows * ceil(V / 4096) < 2^24.
+ *   - No float atomics: repeated calls give the same bits.
+ *   - ws: de_scores_workspace_bytes(rows, V, m) bytes (m = 0 for
+ *     de_topk_distill), 256-byte aligned, in any state: nothing in it outlives a
+ *     call.  Calls that share it must not run concurrently. */
+
+/* Most alternatives of a row, and most entries of a teacher's list. */
+#define DE_TOP_MAX 128
+/* Floats a row of de_token_scores' stats has, and of de_topk_distill's state
+ * beside one for each entry. */
+#define DE_SCORE_STATS 4
+#define DE_DISTILL_STATE 4
+
+/* Incoming gradients of a vocabulary call, and where the logits' gradient goes:
+ * dlogits [rows, ldd], first V of each row, of the logits' type and alignment
+ * (the rest of a row is left as it is).  dlogits may be logits itself (then
+ * ldd == ld) and must not overlap them otherwise.  A row whose incoming
+ * gradients are all zero gets zeros, whatever its logits hold. */
+typedef struct de_row_grad {
+  const float* g;         /* device [rows]: of logp, or of the loss */
+  const float* g_entropy; /* device [rows] or NULL: of the entropy (token scores only);
+                             without g, the entropy's gradient alone */
+  void* dlogits;          /* device */
+  int32_t ldd;
+} de_row_grad;
+
+/* Scratch bytes of de_token_scores with m alternatives, and with m = 0 of
+ * de_topk_distill (0 on invalid sizes). */
+size_t de_scores_workspace_bytes(int rows, int V, int m);
+
+/* Log probabilities of given tokens, entropies and best alternatives:
+ *   logp [rows] = log p[tokens[r]] (tokens int32 [rows]); a negative token marks
+ *     a row without one (logp 0, no gradient), one of V or more gives NaN;
+ *   entropy [rows] = -sum_v p_v log p_v;
+ *   top_idx, top_logp [rows, m], m <= min(V, DE_TOP_MAX): the m most likely
+ *     tokens in descending order, ties to the lower id, and their log
+ *     probabilities (the ids and values of de_topk_distill with tail = 1);
+ *   stats [rows, DE_SCORE_STATS] = (max logit, sum_v exp((l_v - max) / tau),
+ *     entropy, log sum_v exp(l_v / tau)), for de_token_scores_grad.
+ * Each output but one may be NULL (m = 0: no alternatives).  With grad the
+ * logits' gradient comes out of the same call (m must then be 0, else
+ * DE_ERR_UNSUPPORTED):
+ *   dlogits_v = (g (1[v = token] - p_v) - g_entropy p_v (log p_v + entropy)) / tau.
+ * A NaN logit counts as -infinity.  A row with no logit above -infinity, or with
+ * an infinite one, has no distribution: its logp, entropy, top_logp and gradient
+ * are NaN (its top_idx are in order). */
+int de_token_scores(int rows, int V, int dtype, const void* logits, int ld, float tau,
+                    const int32_t* tokens, float* logp, float* entropy, int m, int32_t* top_idx,
+                    float* top_logp, float* stats, const de_row_grad* grad, void* ws,
+                    size_t ws_bytes, hipStream_t stream);
+
+/* The gradient alone, from the same logits, tau and tokens and the stats that
+ * de_token_scores gave for them (tokens may be NULL without g). */
+int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld, float tau,
+                         const int32_t* tokens, const float* stats, const de_row_grad* grad,
+                         hipStream_t stream);
+
+/* Distillation from a teacher's list of m entries a row (m <= DE_TOP_MAX), ids
+ * int32 [rows, m] and values fp32 [rows, m]; q = softmax(logits / tau):
+ *   tail = 0: values are teacher logits, p = softmax(values / tau) over the entries,
+ *     loss[r] = tau^2 sum_S p_j (log p_j - log q_j);
+ *   tail = 1: values are teacher log probabilities at tau, p = exp(values), and the
+ *     tokens outside the list count as one: with P = max(0, 1 - sum_S p_j) and
+ *     Q = sum_{v not in S} q_v, loss[r] = tau^2 (sum_S p_j (log p_j - log q_j)
+ *     + P (log P - log Q)).  The last term is left out where the student gives the
+ *     tokens outside the list no mass at all (the list holds the vocabulary, or
+ *     the others are -infinity).
+ * An id outside [0, V) (such as -1) and an id that an earlier slot of its row holds
+ * are no entries: their values do not count.  A row without entries has loss 0 and a
+ * zero gradient, whatever its logits hold.  A NaN or +infinity among a row's logits,
+ * or in an entry's value, gives a NaN loss and gradient, and so does a list of
+ * -infinities with tail = 0; an entry with p_j = 0 adds nothing, one with p_j > 0 and
+ * a logit of -infinity gives an infinite loss.
+ *   state [rows, m + DE_DISTILL_STATE] (may be NULL): for de_topk_distill_grad;
+ *   grad (may be NULL): the logits' gradient out of the same call,
+ *     dlogits_v = g tau (q_v - p_v) for entries, g tau q_v (1 - P / Q) for the other
+ *     tokens (P = 0 with tail = 0). */
+int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int m,
+                    const int32_t* ids, const float* values, int tail, float tau, float* loss,
+                    float* state, const de_row_grad* grad, void* ws, size_t ws_bytes,
+                    hipStream_t stream);
+
+/* The gradient alone, from the same logits, ids and tau and the state that
+ * de_topk_distill gave for them. */
+int de_topk_distill_grad(int rows, int V, int dtype, const void* logits, int ld, int m,
+                         const int32_t* ids, float tau, const float* state,
+                         const de_row_grad* grad, hipStream_t stream);
+
 /* Pure streaming read of `bytes` (multiple of 16) from buf: the measured HBM
  * read ceiling.  sink [1] receives a value that depends on every byte. */
 int de_stream_probe(const void* buf, size_t bytes, float* sink, hipStream_t stream);

@@ -8,6 +8,7 @@ import of this module fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -50,6 +51,8 @@ C_FUNCS = [
     "de_residual_target", "de_layer_router_logits", "de_row_kl", "de_distill_signals",
     "de_layer_status", "de_model_status", "de_noalloc_scratch_bytes", "de_verify_layer_noalloc",
     "de_verify_single_launch",
+    "de_scores_workspace_bytes", "de_token_scores", "de_token_scores_grad", "de_topk_distill",
+    "de_topk_distill_grad",
 ]
 DE_PHASE_GATEUP = 0
 DE_PHASE_DOWN = 1
@@ -60,6 +63,9 @@ DE_DRAFT = 1
 DE_NEED_DRAFT = 0
 DE_NEED_VERIFY = 1
 DE_BUDGET_CACHE = -1
+DE_TOP_MAX = 128
+DE_SCORE_STATS = 4
+DE_DISTILL_STATE = 4
 
 
 class DEError(RuntimeError):
@@ -124,6 +130,11 @@ class TruncCfg(ctypes.Structure):
                 ("prefetch", ctypes.c_int32)]
 
 
+class RowGrad(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("g_entropy", ctypes.c_void_p),
+                ("dlogits", ctypes.c_void_p), ("ldd", ctypes.c_int32)]
+
+
 class CacheCounts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in CACHE_COUNTS] + [
         ("stall_us", ctypes.c_double), ("draft_layers", ctypes.c_int64),
@@ -146,6 +157,7 @@ def _load(path: str = LIB_PATH, strict: bool = True):
     CP = ctypes.POINTER(CacheCfg)
     KP = ctypes.POINTER(CacheCounts)
     I32P = ctypes.POINTER(ctypes.c_int32)
+    GP = ctypes.POINTER(RowGrad)
     sig = {
         "de_abi_version": (I, []),
         "de_error_string": (ctypes.c_char_p, [I]),
@@ -162,6 +174,11 @@ def _load(path: str = LIB_PATH, strict: bool = True):
         "de_layer_router_logits": (I, [DP, I, P, SZ, P, P]),
         "de_row_kl": (I, [I, I, P, I, P, I, P, I, F, P, P, P]),
         "de_distill_signals": (I, [MP, I, P, F, P, P, P, P, P, SZ, P]),
+        "de_scores_workspace_bytes": (SZ, [I, I, I]),
+        "de_token_scores": (I, [I, I, I, P, I, F, P, P, P, I, P, P, P, GP, P, SZ, P]),
+        "de_token_scores_grad": (I, [I, I, I, P, I, F, P, P, GP, P]),
+        "de_topk_distill": (I, [I, I, I, P, I, I, P, P, I, F, P, P, GP, P, SZ, P]),
+        "de_topk_distill_grad": (I, [I, I, I, P, I, I, P, F, P, GP, P]),
         "de_verify_layer": (I, [DP, I, P, P, P, TP, P, P, P, P, P, P, P, P, P, P, EP, P, SZ, P]),
         "de_accept_workspace_bytes": (SZ, [I, I]),
         "de_accept_len": (I, [I, I, P, P, P, P, P, SZ, P]),
@@ -594,3 +611,64 @@ def de_distill_signals(model, T, tokens, tau, m_star, router_kl, logit_kl, token
         ctypes.byref(model), int(T), _ptr(tokens), float(tau), _ptr(m_star), _ptr(router_kl),
         _ptr(logit_kl), _ptr(token_ce), _ptr(ws), ws.numel() if ws is not None else 0,
         _stream(stream)))
+
+
+def de_scores_workspace_bytes(rows, V, m=0) -> int:
+    return LIB.de_scores_workspace_bytes(int(rows), int(V), int(m))
+
+
+def scores_workspace(rows, V, m=0, device="cuda"):
+    """Scratch for de_token_scores with up to m alternatives a row, and for de_topk_distill."""
+    n = de_scores_workspace_bytes(rows, V, m)
+    if n == 0:
+        _check("de_scores_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def make_row_grad(g, dlogits, ldd, g_entropy=None) -> RowGrad:
+    r = RowGrad(_ptr(g), _ptr(g_entropy), _ptr(dlogits), int(ldd))
+    r._keep = (g, dlogits, g_entropy)
+    return r
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def _device_of(t):
+    """The tensor's device as the current one, for a launch on one of its streams."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+        return torch.cuda.device(t.device)
+    return contextlib.nullcontext()
+
+
+def de_token_scores(rows, V, dtype, logits, ld, tau, tokens=None, logp=None, entropy=None, m=0,
+                    top_idx=None, top_logp=None, stats=None, grad=None, ws=None, stream=None):
+    with _device_of(logits):
+        _check("de_token_scores", LIB.de_token_scores(
+            int(rows), int(V), int(dtype), _ptr(logits), int(ld), float(tau), _ptr(tokens), _ptr(logp),
+            _ptr(entropy), int(m), _ptr(top_idx), _ptr(top_logp), _ptr(stats), _ref(grad), _ptr(ws),
+            ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+def de_token_scores_grad(rows, V, dtype, logits, ld, tau, tokens, stats, grad, stream=None):
+    with _device_of(logits):
+        _check("de_token_scores_grad", LIB.de_token_scores_grad(
+            int(rows), int(V), int(dtype), _ptr(logits), int(ld), float(tau), _ptr(tokens),
+            _ptr(stats), _ref(grad), _stream(stream)))
+
+
+def de_topk_distill(rows, V, dtype, logits, ld, m, ids, values, tail, tau, loss, state=None,
+                    grad=None, ws=None, stream=None):
+    with _device_of(logits):
+        _check("de_topk_distill", LIB.de_topk_distill(
+            int(rows), int(V), int(dtype), _ptr(logits), int(ld), int(m), _ptr(ids), _ptr(values),
+            int(tail), float(tau), _ptr(loss), _ptr(state), _ref(grad), _ptr(ws),
+            ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+def de_topk_distill_grad(rows, V, dtype, logits, ld, m, ids, tau, state, grad, stream=None):
+    with _device_of(logits):
+        _check("de_topk_distill_grad", LIB.de_topk_distill_grad(
+            int(rows), int(V), int(dtype), _ptr(logits), int(ld), int(m), _ptr(ids), float(tau),
+            _ptr(state), _ref(grad), _stream(stream)))

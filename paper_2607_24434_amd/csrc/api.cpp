@@ -4,6 +4,7 @@
 #include "de_common.h"
 #include "draft_persistent.h"
 #include "grouped_mfma.h"
+#include "scores.h"
 #include "verify_fused.h"
 
 #include <algorithm>
@@ -1389,6 +1390,146 @@ int de_row_kl(int rows, int n, const float* a, int lda, const float* b, int ldb,
   r.kl = kl;
   r.ce = ce;
   return hip_status(de::launch_rowkl(r, stream));
+}
+
+namespace {
+
+// The scratch of one row of the vocabulary calls.
+size_t scores_row_bytes(int V, int m) {
+  (void)V;
+  (void)m;
+  return (DE_TOP_MAX + DE_DISTILL_STATE) * 4;
+}
+
+int vocab_rows(int rows, int V, int dtype, const void* logits, int ld, float tau,
+               de::VocabRows* x) {
+  if (dtype != DE_F32 && dtype != DE_BF16) return DE_ERR_UNSUPPORTED;
+  if (rows < 1 || rows > (1 << 20) || V < 1 || V > (1 << 30) || ld < V) return DE_ERR_INVALID;
+  // A scale whose exponent constants are normal floats.
+  if (!(tau >= 1e-30f && tau <= 1e30f)) return DE_ERR_INVALID;
+  const uintptr_t mask = dtype == DE_BF16 ? 1 : 3;
+  if (!logits || (reinterpret_cast<uintptr_t>(logits) & mask) != 0) return DE_ERR_INVALID;
+  // A launch has less than 2^32 threads; no memory holds logits for more.
+  if ((int64_t)rows * ((V + 4095) / 4096) >= (1 << 24)) return DE_ERR_UNSUPPORTED;
+  x->rows = rows;
+  x->V = V;
+  x->bf16 = dtype == DE_BF16;
+  x->logits = logits;
+  x->ld = ld;
+  x->tau = tau;
+  const double c = 1.4426950408889634074 / (double)tau;
+  x->c_hi = (float)c;
+  x->c_lo = (float)(c - (double)x->c_hi);
+  x->floor = (float)(-1000. / c);
+  return DE_OK;
+}
+
+// `entropy`: the call has an entropy, whose gradient may come alone.
+int row_grad(const de::VocabRows& x, const de_row_grad* grad, bool entropy, de::RowGrad* g) {
+  const uintptr_t mask = x.bf16 ? 1 : 3;
+  if (!grad->dlogits || (reinterpret_cast<uintptr_t>(grad->dlogits) & mask) != 0 ||
+      grad->ldd < x.V)
+    return DE_ERR_INVALID;
+  if (grad->g_entropy != nullptr && !entropy) return DE_ERR_INVALID;
+  if (grad->g == nullptr && grad->g_entropy == nullptr) return DE_ERR_INVALID;
+  // In place only row by row.
+  if (grad->dlogits == x.logits && grad->ldd != x.ld) return DE_ERR_INVALID;
+  g->g = grad->g;
+  g->g_entropy = grad->g_entropy;
+  g->dlogits = grad->dlogits;
+  g->ldd = grad->ldd;
+  return DE_OK;
+}
+
+int check_scores_ws(int rows, int V, int m, const void* ws, size_t ws_bytes) {
+  if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0 ||
+      ws_bytes < de_scores_workspace_bytes(rows, V, m))
+    return DE_ERR_WORKSPACE;
+  return DE_OK;
+}
+
+}  // namespace
+
+size_t de_scores_workspace_bytes(int rows, int V, int m) {
+  if (rows < 1 || rows > (1 << 20) || V < 1 || V > (1 << 30) || m < 0 || m > DE_TOP_MAX) return 0;
+  return up256(rows * scores_row_bytes(V, m));
+}
+
+int de_token_scores(int rows, int V, int dtype, const void* logits, int ld, float tau,
+                    const int32_t* tokens, float* logp, float* entropy, int m, int32_t* top_idx,
+                    float* top_logp, float* stats, const de_row_grad* grad, void* ws,
+                    size_t ws_bytes, hipStream_t stream) {
+  de::ScoresArgs a{};
+  de::RowGrad g{};
+  int rc = vocab_rows(rows, V, dtype, logits, ld, tau, &a.x);
+  if (rc != DE_OK) return rc;
+  if (m < 0 || m > DE_TOP_MAX || m > V) return DE_ERR_INVALID;
+  if ((logp != nullptr && !tokens) || (m > 0 && (!top_idx || !top_logp))) return DE_ERR_INVALID;
+  if (!logp && !entropy && !stats && m == 0 && !grad) return DE_ERR_INVALID;
+  if (grad != nullptr) {
+    if ((rc = row_grad(a.x, grad, true, &g)) != DE_OK) return rc;
+    if (grad->g != nullptr && !tokens) return DE_ERR_INVALID;
+    if (m > 0) return DE_ERR_UNSUPPORTED;
+  }
+  if ((rc = check_scores_ws(rows, V, m, ws, ws_bytes)) != DE_OK) return rc;
+  a.tokens = tokens;
+  a.logp = logp;
+  a.entropy = entropy;
+  a.m = m;
+  a.top_idx = top_idx;
+  a.top_logp = top_logp;
+  a.stats = stats;
+  if (grad != nullptr && stats == nullptr) a.stats = static_cast<float*>(ws);
+  if ((rc = hip_status(de::launch_scores(a, stream))) != DE_OK || grad == nullptr) return rc;
+  return hip_status(de::launch_scores_grad(a.x, tokens, a.stats, g, stream));
+}
+
+int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld, float tau,
+                         const int32_t* tokens, const float* stats, const de_row_grad* grad,
+                         hipStream_t stream) {
+  de::VocabRows x{};
+  de::RowGrad g{};
+  int rc = vocab_rows(rows, V, dtype, logits, ld, tau, &x);
+  if (rc != DE_OK) return rc;
+  if (!stats || !grad) return DE_ERR_INVALID;
+  if ((rc = row_grad(x, grad, true, &g)) != DE_OK) return rc;
+  if (grad->g != nullptr && !tokens) return DE_ERR_INVALID;
+  return hip_status(de::launch_scores_grad(x, tokens, stats, g, stream));
+}
+
+int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int m,
+                    const int32_t* ids, const float* values, int tail, float tau, float* loss,
+                    float* state, const de_row_grad* grad, void* ws, size_t ws_bytes,
+                    hipStream_t stream) {
+  de::DistillArgs a{};
+  de::RowGrad g{};
+  int rc = vocab_rows(rows, V, dtype, logits, ld, tau, &a.x);
+  if (rc != DE_OK) return rc;
+  if (m < 1 || m > DE_TOP_MAX || !ids || !values || !loss) return DE_ERR_INVALID;
+  if (tail != 0 && tail != 1) return DE_ERR_UNSUPPORTED;
+  if (grad != nullptr && (rc = row_grad(a.x, grad, false, &g)) != DE_OK) return rc;
+  if ((rc = check_scores_ws(rows, V, 0, ws, ws_bytes)) != DE_OK) return rc;
+  a.m = m;
+  a.ids = ids;
+  a.values = values;
+  a.tail = tail;
+  a.loss = loss;
+  a.state = state;
+  if (grad != nullptr && state == nullptr) a.state = static_cast<float*>(ws);
+  if ((rc = hip_status(de::launch_distill(a, stream))) != DE_OK || grad == nullptr) return rc;
+  return hip_status(de::launch_distill_grad(a.x, m, ids, a.state, g, stream));
+}
+
+int de_topk_distill_grad(int rows, int V, int dtype, const void* logits, int ld, int m,
+                         const int32_t* ids, float tau, const float* state,
+                         const de_row_grad* grad, hipStream_t stream) {
+  de::VocabRows x{};
+  de::RowGrad g{};
+  int rc = vocab_rows(rows, V, dtype, logits, ld, tau, &x);
+  if (rc != DE_OK) return rc;
+  if (m < 1 || m > DE_TOP_MAX || !ids || !state || !grad) return DE_ERR_INVALID;
+  if ((rc = row_grad(x, grad, false, &g)) != DE_OK) return rc;
+  return hip_status(de::launch_distill_grad(x, m, ids, state, g, stream));
 }
 
 int de_stream_probe(const void* buf, size_t bytes, float* sink, hipStream_t stream) {
