@@ -1394,12 +1394,9 @@ int de_row_kl(int rows, int n, const float* a, int lda, const float* b, int ldb,
 
 namespace {
 
-// The scratch of one row of the vocabulary calls.
-size_t scores_row_bytes(int V, int m) {
-  (void)V;
-  (void)m;
-  return (DE_TOP_MAX + DE_DISTILL_STATE) * 4;
-}
+// The scratch of a vocabulary call: what its launches exchange, then the rows' statistics
+// or state where the caller keeps none.
+size_t scores_state_at(int rows, int V, int m) { return up256(de::scores_bytes(rows, V, m)); }
 
 int vocab_rows(int rows, int V, int dtype, const void* logits, int ld, float tau,
                de::VocabRows* x) {
@@ -1419,7 +1416,8 @@ int vocab_rows(int rows, int V, int dtype, const void* logits, int ld, float tau
   x->tau = tau;
   const double c = 1.4426950408889634074 / (double)tau;
   x->c_hi = (float)c;
-  x->c_lo = (float)(c - (double)x->c_hi);
+  if ((double)x->c_hi >= c) x->c_hi = std::nextafter(x->c_hi, 0.f);
+  x->c_lo = std::max((float)(c - (double)x->c_hi), 1.2e-38f);
   x->floor = (float)(-1000. / c);
   return DE_OK;
 }
@@ -1452,7 +1450,7 @@ int check_scores_ws(int rows, int V, int m, const void* ws, size_t ws_bytes) {
 
 size_t de_scores_workspace_bytes(int rows, int V, int m) {
   if (rows < 1 || rows > (1 << 20) || V < 1 || V > (1 << 30) || m < 0 || m > DE_TOP_MAX) return 0;
-  return up256(rows * scores_row_bytes(V, m));
+  return scores_state_at(rows, V, m) + up256((size_t)rows * (DE_TOP_MAX + DE_DISTILL_STATE) * 4);
 }
 
 int de_token_scores(int rows, int V, int dtype, const void* logits, int ld, float tau,
@@ -1479,8 +1477,8 @@ int de_token_scores(int rows, int V, int dtype, const void* logits, int ld, floa
   a.top_idx = top_idx;
   a.top_logp = top_logp;
   a.stats = stats;
-  if (grad != nullptr && stats == nullptr) a.stats = static_cast<float*>(ws);
-  if ((rc = hip_status(de::launch_scores(a, stream))) != DE_OK || grad == nullptr) return rc;
+  if (grad != nullptr && stats == nullptr) a.stats = at<float>(ws, scores_state_at(rows, V, m));
+  if ((rc = hip_status(de::launch_scores(a, ws, stream))) != DE_OK || grad == nullptr) return rc;
   return hip_status(de::launch_scores_grad(a.x, tokens, a.stats, g, stream));
 }
 
@@ -1515,8 +1513,8 @@ int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int 
   a.tail = tail;
   a.loss = loss;
   a.state = state;
-  if (grad != nullptr && state == nullptr) a.state = static_cast<float*>(ws);
-  if ((rc = hip_status(de::launch_distill(a, stream))) != DE_OK || grad == nullptr) return rc;
+  if (grad != nullptr && state == nullptr) a.state = at<float>(ws, scores_state_at(rows, V, 0));
+  if ((rc = hip_status(de::launch_distill(a, ws, stream))) != DE_OK || grad == nullptr) return rc;
   return hip_status(de::launch_distill_grad(a.x, m, ids, a.state, g, stream));
 }
 

@@ -12,9 +12,9 @@ constexpr int kStats = 4;     // floats a row of token scores keeps for its grad
 constexpr int kState = 4;     // floats a distillation row keeps beside one per entry
 
 // The rows that every call reads, and the scale of their softmax: exp((l - max) / tau)
-// is exp2((l - max) * (c_hi + c_lo)), log2(e) / tau in two floats.  One float's rounding
-// would move every term of a far logit the same way (by |l - max| 2^-25), and a loss
-// is a small difference of such sums.
+// is exp2((l - max) * (c_hi + c_lo)), log2(e) / tau in two floats, c_lo > 0.  One float's
+// rounding would move every term of a far logit the same way (by |l - max| 2^-25), and
+// a loss is a small difference of such sums.
 struct VocabRows {
   int rows, V;
   int bf16;            // 0: fp32 logits
@@ -54,10 +54,12 @@ struct DistillArgs {
   float* state;           // [rows, m + kState] or NULL
 };
 
-hipError_t launch_scores(const ScoresArgs& a, hipStream_t s);
+// Scratch of launch_scores and (m = 0) launch_distill, 16-byte aligned.
+size_t scores_bytes(int rows, int V, int m);
+hipError_t launch_scores(const ScoresArgs& a, void* ws, hipStream_t s);
 hipError_t launch_scores_grad(const VocabRows& x, const int32_t* tokens, const float* stats,
                               const RowGrad& g, hipStream_t s);
-hipError_t launch_distill(const DistillArgs& a, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_distill_grad(const VocabRows& x, int m, const int32_t* ids, const float* state,
                                const RowGrad& g, hipStream_t s);
 

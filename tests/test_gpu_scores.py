@@ -170,7 +170,7 @@ def shapes(V):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("V,m", [(1000, 128), (5000, 20), (40000, 128), (102401, 64)])
+@pytest.mark.parametrize("V,m", [(1000, 128), (5000, 20), (9000, 1), (40000, 128), (102401, 64), (260001, 128)])
 def test_orders_ties_and_masked_logits(V, m, dtype):
     rows = shapes(V)
     x = np.stack(list(rows.values()))

@@ -142,5 +142,10 @@ def test_workspace_sizes():
     assert b(0, 100, 0) == 0 and b(1, 0, 0) == 0 and b(1, 100, -1) == 0 and b(1, 100, 129) == 0
     for V in (1, 1000, 102400, 1 << 30):
         assert 0 < b(1, V, 0) <= b(2, V, 0) and b(1, V, 0) <= b(1, V, 128)
+    # Scratch for more rows serves fewer, however the rows are split.
+    for V in (1000, 9000, 20000, 102400, 260001):
+        for m in (0, 5):
+            sizes = [b(r, V, m) for r in (1, 2, 5, 9, 17, 40, 64, 79, 100, 155, 300, 2048)]
+            assert sizes == sorted(sizes)
     # The scratch is small beside the logits.
     assert b(2048, 102400, 128) < 2048 * 102400 * 4 // 16
