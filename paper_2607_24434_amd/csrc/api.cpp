@@ -1415,10 +1415,8 @@ int vocab_rows(int rows, int V, int dtype, const void* logits, int ld, float tau
   x->ld = ld;
   x->tau = tau;
   const double c = 1.4426950408889634074 / (double)tau;
-  x->c_hi = (float)c;
-  if ((double)x->c_hi >= c) x->c_hi = std::nextafter(x->c_hi, 0.f);
-  x->c_lo = std::max((float)(c - (double)x->c_hi), 1.2e-38f);
-  x->floor = (float)(-1000. / c);
+  x->c = (float)c;
+  x->corr = (float)((c - (double)x->c) / c * 0.69314718055994530942);
   return DE_OK;
 }
 
@@ -1478,8 +1476,7 @@ int de_token_scores(int rows, int V, int dtype, const void* logits, int ld, floa
   a.top_logp = top_logp;
   a.stats = stats;
   if (grad != nullptr && stats == nullptr) a.stats = at<float>(ws, scores_state_at(rows, V, m));
-  if ((rc = hip_status(de::launch_scores(a, ws, stream))) != DE_OK || grad == nullptr) return rc;
-  return hip_status(de::launch_scores_grad(a.x, tokens, a.stats, g, stream));
+  return hip_status(de::launch_scores(a, g, ws, stream));
 }
 
 int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld, float tau,
@@ -1514,8 +1511,7 @@ int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int 
   a.loss = loss;
   a.state = state;
   if (grad != nullptr && state == nullptr) a.state = at<float>(ws, scores_state_at(rows, V, 0));
-  if ((rc = hip_status(de::launch_distill(a, ws, stream))) != DE_OK || grad == nullptr) return rc;
-  return hip_status(de::launch_distill_grad(a.x, m, ids, a.state, g, stream));
+  return hip_status(de::launch_distill(a, g, ws, stream));
 }
 
 int de_topk_distill_grad(int rows, int V, int dtype, const void* logits, int ld, int m,

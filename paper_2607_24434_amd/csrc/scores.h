@@ -11,18 +11,16 @@ constexpr int kTopMax = 128;  // most alternatives, and most entries of a teache
 constexpr int kStats = 4;     // floats a row of token scores keeps for its gradient
 constexpr int kState = 4;     // floats a distillation row keeps beside one per entry
 
-// The rows that every call reads, and the scale of their softmax: exp((l - max) / tau)
-// is exp2((l - max) * (c_hi + c_lo)), log2(e) / tau in two floats, c_lo > 0.  One float's
-// rounding would move every term of a far logit the same way (by |l - max| 2^-25), and
-// a loss is a small difference of such sums.
+// The rows that every call reads, and the scale of their softmax: exp((l - max) / tau) is
+// 2^d with d = (l - max) c, c = log2(e) / tau rounded.  The rounding moves every d the same
+// way, and a loss is a small difference of sums of such terms; to first order, sum 2^d is
+// right with corr * (sum 2^d d) added, a sum that the entropy takes anyway.
 struct VocabRows {
   int rows, V;
   int bf16;            // 0: fp32 logits
   const void* logits;  // [rows, ld]
   int64_t ld;
-  float tau, c_hi, c_lo;
-  float floor;         // differences to the maximum are not let below this: its
-                       // exponential is 0 in fp32, and finite times 0 is 0
+  float tau, c, corr;
 };
 
 // Incoming gradients and where the logits' gradient goes (dlogits NULL: none).
@@ -56,10 +54,11 @@ struct DistillArgs {
 
 // Scratch of launch_scores and (m = 0) launch_distill, 16-byte aligned.
 size_t scores_bytes(int rows, int V, int m);
-hipError_t launch_scores(const ScoresArgs& a, void* ws, hipStream_t s);
+// With g.dlogits the gradient too, for which a.stats (a.state) must not be NULL.
+hipError_t launch_scores(const ScoresArgs& a, const RowGrad& g, void* ws, hipStream_t s);
 hipError_t launch_scores_grad(const VocabRows& x, const int32_t* tokens, const float* stats,
                               const RowGrad& g, hipStream_t s);
-hipError_t launch_distill(const DistillArgs& a, void* ws, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, const RowGrad& g, void* ws, hipStream_t s);
 hipError_t launch_distill_grad(const VocabRows& x, int m, const int32_t* ids, const float* state,
                                const RowGrad& g, hipStream_t s);
 

@@ -1,0 +1,486 @@
+// What the row operators over a vocabulary are made of: a row as 16-byte slots, tiles of it in
+// registers, reductions over a tile and the split of rows into parts.
+//
+// A row is read in tiles: each thread of a block has up to U 16-byte slots of it in
+// registers, all of their loads in flight together, and takes the maximum, the sums and
+// (gradients) the results from there, so that logits are read once.  Slots lie at
+// multiples of 16 bytes whatever element the row starts at; its first and last one may be
+// partly outside it and are then loaded by the element.
+#pragma once
+
+#include "de_common.h"
+#include "scores.h"
+
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+namespace de {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTileU = 8;  // slots a thread of a part of a row
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Rows in parts: what each part leaves for the row's last step, in the caller's scratch.
+struct Split {
+  int chunks;      // parts of a row
+  int nu;          // slots a thread of a part, at most the kernel's U
+  float4* parts;   // [rows, chunks]: maximum, sum e, sum e d
+  float* gm;       // [rows, gstride]: groups' maxima
+  int gstride, glog;
+};
+
+__device__ __forceinline__ float nan_f() { return __int_as_float(0x7fc00000); }
+
+// f(0) ... f(U - 1), the numbers as types.  Not a loop: where f does nothing from some number on,
+// the compiler shortens a loop before it unrolls it, and the tile becomes an array in memory.
+template <int... u, typename F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, u...>, const F& f) {
+  (f(std::integral_constant<int, u>{}), ...);
+}
+template <int U, typename F>
+__device__ __forceinline__ void each(const F& f) {
+  each_of(std::make_integer_sequence<int, U>{}, f);
+}
+
+template <typename T>
+constexpr int kE = 16 / (int)sizeof(T);  // logits of a slot
+
+__device__ __forceinline__ float load1(const float* p) { return *gptr<float>(p); }
+__device__ __forceinline__ float load1(const uint16_t* p) {
+  return __uint_as_float((uint32_t)*gptr<uint16_t>(p) << 16);
+}
+__device__ __forceinline__ uint32_t bf16_bits(float v) {
+  return __builtin_bit_cast(uint16_t, (__bf16)v);  // to nearest, ties to even; a NaN stays one
+}
+__device__ __forceinline__ void store1(float* p, float v) { *(DE_GLOBAL float*)p = v; }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *(DE_GLOBAL uint16_t*)p = (uint16_t)bf16_bits(v); }
+
+// Logit c of a slot.
+template <typename T>
+__device__ __forceinline__ float get(const u32x4& x, int c) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(x[c]);
+  else return c & 1 ? bf16_hi(x[c >> 1]) : bf16_lo(x[c >> 1]);
+}
+// -infinity in its place.
+template <typename T>
+__device__ __forceinline__ void drop(u32x4& x, int c) {
+  if constexpr (sizeof(T) == 4) x[c] = 0xff800000u;
+  else x[c >> 1] = c & 1 ? (x[c >> 1] & 0xffffu) | 0xff800000u : (x[c >> 1] & 0xffff0000u) | 0xff80u;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 all_dropped() {
+  const uint32_t v = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  return u32x4{v, v, v, v};
+}
+template <typename T>
+__device__ __forceinline__ u32x4 packed(const float (&v)[kE<T>]) {
+  u32x4 x;
+  each<4>([&](auto c) __attribute__((always_inline)) {
+    if constexpr (sizeof(T) == 4) x[c.value] = __float_as_uint(v[c]);
+    else x[c.value] = bf16_bits(v[2 * c]) | bf16_bits(v[2 * c + 1]) << 16;
+  });
+  return x;
+}
+
+// A row's slots: element i of the row is logit (i + o) % E of slot (i + o) / E.
+struct Row {
+  const char* base;  // slot 0
+  int V, o;
+  int f0, f1;        // slots wholly inside: [f0, f1)
+  int slots;
+};
+
+template <typename T>
+__device__ __forceinline__ Row row_at(const void* p, int64_t ld, int r, int V) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p) + (uintptr_t)((int64_t)r * ld) * sizeof(T);
+  Row w;
+  w.base = reinterpret_cast<const char*>(a & ~(uintptr_t)15);
+  w.V = V;
+  w.o = (int)(a & 15) / (int)sizeof(T);
+  w.f0 = w.o > 0;
+  w.f1 = (V + w.o) / kE<T>;
+  w.slots = (V + w.o + kE<T> - 1) / kE<T>;
+  return w;
+}
+
+// The row up to slot `end`, for a tile of it.
+__device__ __forceinline__ Row until(Row w, int end) {
+  w.f1 = min(w.f1, end);
+  w.slots = min(w.slots, end);
+  return w;
+}
+
+template <typename T>
+__device__ __forceinline__ const T* elem_at(const Row& w, int i) {
+  return reinterpret_cast<const T*>(w.base) + w.o + i;
+}
+
+// One slot, any of whose elements may be outside the row (-infinity there).  Its elements
+// are loaded whether inside or not, at the nearest place that is, so that their loads do
+// not wait for each other.
+template <typename T>
+__device__ __forceinline__ u32x4 load_edge(const Row& w, int s) {
+  if (s >= w.f0 && s < w.f1) return load_stream16(w.base + (int64_t)s * 16);
+  uint32_t v[kE<T>];
+  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+    const T* p = elem_at<T>(w, min(max(s * kE<T> + c - w.o, 0), w.V - 1));
+    if constexpr (sizeof(T) == 4) v[c] = __float_as_uint(load1(p));
+    else v[c] = *gptr<uint16_t>(p);
+  });
+  u32x4 x;
+  each<4>([&](auto c) __attribute__((always_inline)) {
+    if constexpr (sizeof(T) == 4) x[c.value] = v[c];
+    else x[c.value] = v[2 * c] | v[2 * c + 1] << 16;
+  });
+  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+    const int i = s * kE<T> + c - w.o;
+    if (i < 0 || i >= w.V) drop<T>(x, c);
+  });
+  return x;
+}
+
+// The slots slot0 + u * NTH + thread of a row, u < m in x; slot u = m, in `last`, where the row
+// ends inside a slot: it is loaded by the element, once the others are taken.
+template <int NTH, int U>
+struct Tile {
+  u32x4 x[U];
+  u32x4 last;
+  int slot0, m;
+  bool ragged;
+
+  __device__ __forceinline__ int slot(int u) const { return slot0 + u * NTH + threadIdx.x; }
+};
+
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void load_tile(Tile<NTH, U>& x, const Row& w, int slot0) {
+  x.slot0 = slot0;
+  x.ragged = w.f1 < w.slots && w.slots > slot0;
+  x.m = (w.slots - slot0 + NTH - 1) / NTH - x.ragged;
+  if (x.m > 0 && slot0 < w.f0) x.x[0] = load_edge<T>(w, x.slot(0));
+  each<U>([&](auto u) __attribute__((always_inline)) {
+    if (u >= x.m || (u == 0 && slot0 < w.f0)) return;
+    if (slot0 + (u + 1) * NTH <= w.f1) {
+      x.x[u] = load_stream16(w.base + (int64_t)(slot0 + u * NTH) * 16 + threadIdx.x * 16);
+    } else {
+      x.x[u] = all_dropped<T>();
+      if (x.slot(u) < w.f1) x.x[u] = load_stream16(w.base + (int64_t)x.slot(u) * 16);
+    }
+  });
+}
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void load_last(Tile<NTH, U>& x, const Row& w) {
+  if (!x.ragged) return;
+  x.last = all_dropped<T>();
+  if (x.slot(x.m) < w.slots) x.last = load_edge<T>(w, x.slot(x.m));
+}
+
+// f(slot, u) for every slot of a thread.
+template <int NTH, int U, typename F>
+__device__ __forceinline__ void each_slot(Tile<NTH, U>& x, const F& f) {
+  each<U>([&](auto u) __attribute__((always_inline)) {
+    if (u < x.m) f(x.x[u], (int)u);
+  });
+  if (x.ragged) f(x.last, x.m);
+}
+
+// Writes a slot of results to the row `out`, whose slots are those of w (same offset) or not.
+template <typename T>
+__device__ __forceinline__ void store_slot(const Row& w, const Row& out, int s, const float (&v)[kE<T>]) {
+  if (out.o == w.o && s >= w.f0 && s < w.f1) {
+    *(DE_GLOBAL u32x4*)(out.base + (int64_t)s * 16) = packed<T>(v);
+    return;
+  }
+  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+    const int i = s * kE<T> + c - w.o;
+    if (i >= 0 && i < w.V) store1(const_cast<T*>(elem_at<T>(out, i)), v[c]);
+  });
+}
+
+// Zeros to a row from slot0 on.
+template <typename T, int NTH>
+__device__ __forceinline__ void zero_tile(const Row& w, const Row& out, int slot0) {
+  const float v[kE<T>] = {};
+#pragma unroll 1
+  for (int s = slot0 + threadIdx.x; s < w.slots; s += NTH) store_slot<T>(w, out, s, v);
+}
+
+// log2 of exp((l - top) / tau).  Differences are taken before they are scaled, so that logits
+// far from zero, up to the type's lowest value, lose nothing.
+__device__ __forceinline__ float scaled(const VocabRows& x, float l, float top) { return (l - top) * x.c; }
+// ... not below a value whose power of two is 0 in fp32, and whose product with 0 is 0: also
+// for -infinity, a NaN and an infinity's difference to itself.
+__device__ __forceinline__ float scaled_floor(const VocabRows& x, float l, float top) {
+  return fmaxf(scaled(x, l, top), -1000.f);
+}
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// log p of one logit (a NaN is -infinity).
+__device__ __forceinline__ float log_p(float tau, float l, float top, float log_s) {
+  return l == l ? (l - top) / tau - log_s : log_s == log_s ? -INFINITY : log_s;
+}
+
+// A whole number that orders values as their floats do (a NaN as -infinity, -0 as +0).
+__device__ __forceinline__ uint32_t order_key(float v) {
+  const uint32_t b = __float_as_uint(v == v ? v + 0.f : -INFINITY);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+// ... and the lower index first.
+__device__ __forceinline__ uint64_t order_key(float v, int i) {
+  return (uint64_t)order_key(v) << 32 | (0xffffffffu - (uint32_t)i);
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
+
+// ---------------------------------------------------------------- reductions
+
+template <int ctrl, int rows>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, rows, 0xF, false));
+}
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, dpp<0xB1, 0xF>(v));     // quad_perm 1,0,3,2
+  return fmaxf(v, dpp<0x4E, 0xF>(v));  // quad_perm 2,3,0,1
+}
+__device__ __forceinline__ float row16_max(float v) {
+  v = quad_max(v);
+  v = fmaxf(v, dpp<0x141, 0xF>(v));    // row_half_mirror
+  return fmaxf(v, dpp<0x140, 0xF>(v)); // row_mirror
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = row16_max(v);
+  v = fmaxf(v, dpp<0x142, 0xA>(v));    // row_bcast:15
+  v = fmaxf(v, dpp<0x143, 0xC>(v));    // row_bcast:31
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Over the block; every thread has the result.  `red` (a float for each wave) must not be
+// in use by an earlier reduction that a thread may still read.
+template <int NTH>
+__device__ __forceinline__ float block_max(float v, float* red) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = red[0];
+#pragma unroll
+  for (int w = 1; w < NTH / 64; ++w) t = fmaxf(t, red[w]);
+  return t;
+}
+template <int NTH>
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = red[0];
+#pragma unroll
+  for (int w = 1; w < NTH / 64; ++w) t += red[w];
+  return t;
+}
+
+template <typename Op>
+__device__ __forceinline__ double wave_all(double v, Op op) {
+  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, kWave));
+  return v;
+}
+__device__ __forceinline__ double wave_sum64(double v) {
+  return wave_all(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_max64(double v) {
+  return wave_all(v, [](double a, double b) { return a > b ? a : b; });
+}
+
+// ---------------------------------------------------------------- sums over a tile
+
+// Running sums of a part of a row: its maximum (a NaN left out) and, relative to it, sum e and
+// sum e d (d in log2).  Without any logit above -infinity the differences are to 0.
+struct Part {
+  float top, s, w;
+};
+
+__device__ __forceinline__ float finite_top(float top) { return top == -INFINITY ? 0.f : top; }
+
+// p relative to `top`, at least its own.
+__device__ __forceinline__ Part rebased(const VocabRows& x, const Part& p, float top) {
+  const float d = scaled_floor(x, p.top, finite_top(top)), e = exp2_fast(d);
+  return Part{top, p.s * e, fmaf(p.s, d, p.w) * e};
+}
+
+// A thread's slots in batches of kRun, each as its loads arrive: waiting for all of them
+// and the row's maximum first left the memory idle while the terms were computed.  `fix`
+// may change a slot before it is taken.  With `nan` a NaN makes the sum one, else it
+// counts as -infinity.
+constexpr int kRun = 4;
+
+template <typename T, bool nan, int NTH, int U, typename F>
+__device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, const Row& w, const F& fix) {
+  Part p{-INFINITY, 0.f, 0.f};
+  const auto rise = [&](float& top, const u32x4& s) __attribute__((always_inline)) {
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) { top = fmaxf(top, get<T>(s, c)); });
+  };
+  const auto add = [&](const u32x4& s) __attribute__((always_inline)) {
+    const float t = finite_top(p.top);
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+      const float l = get<T>(s, c), d = scaled_floor(a, l, t), e = exp2_fast(nan ? scaled(a, l, t) : d);
+      p.s += e;
+      p.w = fmaf(e, d, p.w);
+    });
+  };
+  each<(U + kRun - 1) / kRun>([&](auto b) __attribute__((always_inline)) {
+    constexpr int u0 = b * kRun, k = U - u0 < kRun ? U - u0 : kRun;
+    if (u0 >= x.m) return;
+    float top = p.top;
+    each<k>([&](auto i) __attribute__((always_inline)) {
+      if (u0 + i >= x.m) return;
+      fix(x.x[u0 + i], u0 + i);
+      rise(top, x.x[u0 + i]);
+    });
+    p = rebased(a, p, top);
+    each<k>([&](auto i) __attribute__((always_inline)) {
+      if (u0 + i < x.m) add(x.x[u0 + i]);
+    });
+  });
+  if (x.ragged) {
+    load_last<T>(x, w);
+    fix(x.last, x.m);
+    float top = p.top;
+    rise(top, x.last);
+    p = rebased(a, p, top);
+    add(x.last);
+  }
+  return p;
+}
+struct NoFix {
+  __device__ __forceinline__ void operator()(u32x4&, int) const {}
+};
+
+// The parts of a block's threads as one.
+template <int NTH>
+__device__ __forceinline__ Part block_part(const VocabRows& a, Part p, float (*red)[NTH / 64]) {
+  const float top = block_max<NTH>(p.top, red[0]);
+  p = rebased(a, p, top);
+  p.s = block_sum<NTH>(p.s, red[1]);
+  p.w = block_sum<NTH>(p.w, red[2]);
+  return p;
+}
+
+// The maxima of groups of 2^glog slots (0, 2 or 4) of a tile: the best m logits lie in the m
+// groups whose (maximum, lower index) are best, so that only those are looked at again.
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void tile_groups(Tile<NTH, U>& x, const Row& w, int glog, float* gm) {
+  const bool first = (threadIdx.x & ((1 << glog) - 1)) == 0;
+  each_slot(x, [&](const u32x4& s, int u) __attribute__((always_inline)) {
+    float v = -INFINITY;
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) { v = fmaxf(v, get<T>(s, c)); });
+    if (glog == 4) v = row16_max(v);
+    else if (glog == 2) v = quad_max(v);
+    if (first && x.slot(u) < w.slots) gm[x.slot(u) >> glog] = v;
+  });
+}
+
+// Marks of a tile's list entries: a bit for each logit, and for each wave a bit for each of
+// its slots that has one, so that the others cost a scalar test.
+template <typename T, int NTH, int U>
+struct Marks {
+  uint32_t bits[U * NTH * kE<T> / 32];
+  uint32_t slots[NTH / 64][(U + 31) / 32];
+};
+
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void clear_marks(Marks<T, NTH, U>& k) {
+  for (int i = threadIdx.x; i < U * NTH * kE<T> / 32; i += NTH) k.bits[i] = 0;
+  if (threadIdx.x < NTH / 64)
+    for (int i = 0; i < (U + 31) / 32; ++i) k.slots[threadIdx.x][i] = 0;
+}
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void set_mark(Marks<T, NTH, U>& k, const Row& w, int slot0, int id) {
+  if (id < 0 || id >= w.V) return;
+  const int64_t e = (int64_t)id + w.o - (int64_t)slot0 * kE<T>;
+  if (e < 0 || e >= (int64_t)U * NTH * kE<T>) return;
+  const int i = (int)e, s = i / kE<T>, u = s / NTH, wave = s % NTH / 64;
+  atomicOr(&k.bits[i >> 5], 1u << (i & 31));
+  atomicOr(&k.slots[wave][u >> 5], 1u << (u & 31));
+}
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void drop_marked(u32x4& x, int u, const Marks<T, NTH, U>& k) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (!(__builtin_amdgcn_readfirstlane(k.slots[wave][u >> 5]) >> (u & 31) & 1)) return;
+  const int i = (u * NTH + threadIdx.x) * kE<T>;
+  const uint32_t b = k.bits[i >> 5] >> (i & 31);
+  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+    if (b >> c & 1) drop<T>(x, c);
+  });
+}
+
+// ---------------------------------------------------------------- host side
+
+// Slots of a row that starts at any element, and of the longest of these rows.
+template <typename T>
+inline int slots_most(int V) {
+  return (V + 2 * (kE<T> - 1)) / kE<T>;
+}
+template <typename T>
+inline int slots_most(const VocabRows& x) {
+  const bool whole = (reinterpret_cast<uintptr_t>(x.logits) & 15u) == 0 && x.ld % kE<T> == 0;
+  return whole ? (x.V + kE<T> - 1) / kE<T> : slots_most<T>(x.V);
+}
+
+// f with the smallest U that holds u slots a thread.
+template <typename F>
+inline void by_u(int u, const F& f) {
+  if (u > 4) f(std::integral_constant<int, 8>{});
+  else if (u > 2) f(std::integral_constant<int, 4>{});
+  else if (u > 1) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 1>{});
+}
+
+// Blocks that few rows are split into: four for each CU.
+constexpr int kBlocks = 1024;
+
+inline int group_log(int slots) { return slots <= 2048 ? 0 : slots <= 8192 ? 2 : 4; }
+
+// Parts of kTileU slots a thread, or of fewer where that would leave CUs without one.
+template <typename T>
+inline Split split_of(const VocabRows& x, int m, void* ws) {
+  Split sp{};
+  const int rows = x.rows, slots = slots_most<T>(x), slabs = (slots + kThreads - 1) / kThreads;
+  int chunks = (slabs + kTileU - 1) / kTileU;
+  if (rows < kBlocks) chunks = std::max(chunks, std::min(slabs, (kBlocks + rows - 1) / rows));
+  sp.nu = (slabs + chunks - 1) / chunks;
+  sp.chunks = (slabs + sp.nu - 1) / sp.nu;
+  sp.glog = group_log(slots);
+  sp.gstride = m > 0 ? (slots >> sp.glog) + 1 : 0;
+  sp.parts = static_cast<float4*>(ws);
+  sp.gm = reinterpret_cast<float*>(sp.parts + (int64_t)rows * sp.chunks);
+  return sp;
+}
+
+// Whole rows in one block's registers, which then write the gradient too: logits are read
+// once and gradients written once.  Threads and slots a thread; at most 512 threads of 256
+// registers, 50 slots of them the row's (102400 fp32 logits).
+constexpr int kWholeSlots = 512 * 50;
+
+template <int NTH, int U>
+struct Whole {
+  static constexpr int kNth = NTH, kU = U;
+};
+// f with the smallest block that holds the slots.
+template <typename F>
+inline void by_whole(int slots, const F& f) {
+  if (slots <= 256) f(Whole<256, 1>{});
+  else if (slots <= 256 * 2) f(Whole<256, 2>{});
+  else if (slots <= 256 * 4) f(Whole<256, 4>{});
+  else if (slots <= 256 * 8) f(Whole<256, 8>{});
+  else if (slots <= 256 * 16) f(Whole<256, 16>{});
+  else if (slots <= 512 * 16) f(Whole<512, 16>{});
+  else if (slots <= 512 * 20) f(Whole<512, 20>{});
+  else f(Whole<512, 50>{});
+}
+// Waves of a SIMD that a block's registers leave room for.
+constexpr int whole_waves(int nth, int u) { return u <= 20 ? 4 : nth / 256; }
+
+inline bool whole_row(int rows, int slots) {
+  return slots <= kWholeSlots && (slots <= kTileU * kThreads || rows >= 128);
+}
+
+}  // namespace
+}  // namespace de

@@ -1,0 +1,452 @@
+// Token scores, forward and backward.
+//
+// With M = max l and S = sum_v exp((l_v - M) / tau):
+//   log p_v = (l_v - M) / tau - log S,     H = log S - (sum_v e_v d_v) / S
+// (e_v the summand, d_v = (l_v - M) / tau).  Differences to the maximum are taken before
+// they are scaled, so that logits far from zero lose nothing.
+#include "scores_core.h"
+
+namespace de {
+namespace {
+
+// ---------------------------------------------------------------- the best m
+
+constexpr int kGroupCap = 1024;         // groups looked at again
+constexpr int kListCap = 9 * kThreads;  // logits: at least m + one round's of a block
+constexpr int kSlack = 16;              // how many more than m a threshold may let through
+constexpr int kBatch = 8;               // slots a thread loads at once
+
+struct TopShared {
+  uint64_t groups[kGroupCap];
+  uint64_t list[kListCap];
+  uint64_t bound;
+  int ngroups, n, need, through;
+  int red[2][kThreads / 64];
+};
+
+// The m best of list[0, n), n > m: moved to its front in no order, n set to m; returns the
+// least of them.  Keys differ, so that some bound lets exactly m through.
+template <int CAP>
+__device__ __attribute__((noinline)) uint64_t prune(uint64_t* list, int& n_shared, int m, TopShared& sh) {
+  constexpr int Q = CAP / kThreads;
+  __syncthreads();
+  const int n = n_shared;
+  uint64_t v[Q], hi = 0, lo = ~0ull;
+#pragma unroll
+  for (int i = 0; i < Q; ++i) {
+    const int j = i * kThreads + threadIdx.x;
+    v[i] = j < n ? list[j] : 0;
+  }
+  // 64 bits from the top: the largest bound with m or more at or over it.
+  lo = 0;
+  int it = 0;
+  for (int b = 63; b >= 0; --b) {
+    hi = lo | 1ull << b;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) c += __popcll(__ballot(v[i] >= hi));
+    if ((threadIdx.x & 63) == 0) sh.red[it & 1][threadIdx.x >> 6] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) c += sh.red[it & 1][w];
+    ++it;
+    if (c >= m) lo = hi;
+    if (c == m) break;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) n_shared = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < Q; ++i)
+    if (v[i] >= lo && v[i] != 0) list[atomicAdd(&n_shared, 1)] = v[i];
+  __syncthreads();
+  return lo;
+}
+
+// The best m of a row in descending order, ties to the lower index, from its groups' maxima
+// gm[0, G) (a block of kThreads threads).
+//   1. Each thread's best group; a bound that m to m + kSlack of the threads reach, by
+//      bisection in one wave.  At least m groups are at or over it.
+//   2. Those groups' logits at or over the bound's value go to a list; both lists are
+//      pruned to their best m whenever they could overflow (rows of many equal or sorted
+//      logits).
+//   3. Each logit's rank in the list is its place.
+template <typename T>
+__device__ void top_select(const Row& w, const float* gm, int G, int glog, int m, float tau, float top,
+                           float log_s, int32_t* idx, float* logp, TopShared& sh) {
+  const int tid = threadIdx.x;
+  uint64_t best = 0;
+  for (int g = tid; g < G; g += kThreads) {
+    const uint64_t k = order_key(gm[g], g);
+    best = k > best ? k : best;
+  }
+  sh.list[tid] = best;
+  if (tid == 0) sh.ngroups = sh.n = 0;
+  __syncthreads();
+  if (tid < kWave) {
+    uint64_t v[kThreads / kWave];
+#pragma unroll
+    for (int i = 0; i < kThreads / kWave; ++i) v[i] = sh.list[i * kWave + tid];
+    const auto count = [&](uint64_t b) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kThreads / kWave; ++i) c += __popcll(__ballot(v[i] >= b));
+      return c;
+    };
+    uint64_t lo = 1;
+    int c = count(lo);
+    if (c > m + kSlack) {
+      lo = 0;
+      for (int b = 63; b >= 0; --b) {
+        const uint64_t mid = lo | 1ull << b;
+        const int k = count(mid);
+        if (k < m) continue;
+        lo = mid;
+        c = k;
+        if (k <= m + kSlack) break;
+      }
+    }
+    if (tid == 0) {
+      sh.bound = lo;
+      sh.through = c;
+    }
+  }
+  __syncthreads();
+  uint64_t bound = sh.bound;
+  const int rounds = (G + kThreads - 1) / kThreads;
+  const bool fits = (int64_t)sh.through * rounds <= kGroupCap;
+  for (int i = 0; i < rounds; ++i) {
+    if (!fits) {
+      __syncthreads();
+      const bool full = sh.ngroups + kThreads > kGroupCap;
+      __syncthreads();  // every thread has read it before one appends
+      if (full) bound = prune<kGroupCap>(sh.groups, sh.ngroups, m, sh);
+    }
+    const int g = i * kThreads + tid;
+    const uint64_t k = g < G ? order_key(gm[g], g) : 0;
+    if (k >= bound) sh.groups[atomicAdd(&sh.ngroups, 1)] = k;
+  }
+  __syncthreads();
+  const int work = sh.ngroups << glog;
+  // A logit of the bound's value may beat the bound's group: only its value counts.
+  bound = bound >> 32 << 32;
+  for (int j0 = 0; j0 < work; j0 += kBatch * kThreads) {
+    u32x4 x[kBatch];
+    int first[kBatch];
+    each<kBatch>([&](auto b) __attribute__((always_inline)) {
+      const int j = j0 + b * kThreads + tid;
+      x[b] = all_dropped<T>();
+      first[b] = INT32_MIN / 2;
+      if (j < work) {
+        const int s = (key_index(sh.groups[j >> glog]) << glog) + (j & ((1 << glog) - 1));
+        if (s < w.slots) {
+          x[b] = load_edge<T>(w, s);
+          first[b] = s * kE<T> - w.o;
+        }
+      }
+    });
+    // A bit for each logit at or over the bound.
+    uint32_t take[kBatch];
+    int mine = 0;
+    each<kBatch>([&](auto b) __attribute__((always_inline)) {
+      take[b] = 0;
+      each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+        const int i = first[b] + c;
+        if (i >= 0 && i < w.V && order_key(get<T>(x[b], c), i) >= bound) take[b] |= 1u << c;
+      });
+      mine += __popc(take[b]);
+    });
+    if (tid == 0) sh.need = 0;
+    __syncthreads();
+    if (mine) atomicAdd(&sh.need, mine);
+    __syncthreads();
+    const bool room = sh.n + sh.need <= kListCap;
+    __syncthreads();
+    if (room) {
+      int at = mine ? atomicAdd(&sh.n, mine) : 0;
+      each<kBatch>([&](auto b) __attribute__((always_inline)) {
+        if (take[b] == 0) return;
+        each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+          if (take[b] >> c & 1) sh.list[at++] = order_key(get<T>(x[b], c), first[b] + c);
+        });
+      });
+    } else {
+      // One logit a thread at a time, read again.
+#pragma unroll 1
+      for (int b = 0; b < kBatch; ++b)
+#pragma unroll 1
+        for (int c = 0; c < kE<T>; ++c) {
+          __syncthreads();
+          const bool full = sh.n + kThreads > kListCap;
+          __syncthreads();  // every thread has read it before one appends
+          if (full) bound = prune<kListCap>(sh.list, sh.n, m, sh);
+          const int j = j0 + b * kThreads + tid;
+          if (j >= work) continue;
+          const int i = ((key_index(sh.groups[j >> glog]) << glog) + (j & ((1 << glog) - 1))) * kE<T> - w.o + c;
+          if (i < 0 || i >= w.V) continue;
+          const uint64_t k = order_key(load1(elem_at<T>(w, i)), i);
+          if (k >= bound) sh.list[atomicAdd(&sh.n, 1)] = k;
+        }
+    }
+    __syncthreads();
+  }
+  if (sh.n > kThreads) prune<kListCap>(sh.list, sh.n, m, sh);
+  const int n = sh.n;
+  if (tid >= n) return;
+  const uint64_t mine = sh.list[tid];
+  int rank = 0;
+  for (int i = 0; i < n; ++i) rank += sh.list[i] > mine;
+  if (rank >= m) return;
+  const int i = key_index(mine);
+  idx[rank] = i;
+  logp[rank] = log_p(tau, load1(elem_at<T>(w, i)), top, log_s);
+}
+
+// ---------------------------------------------------------------- token scores
+
+struct RowScore {
+  float top, s, h, log_s;
+};
+
+__device__ __forceinline__ RowScore row_score(const VocabRows& x, const Part& p) {
+  RowScore r;
+  r.top = p.top;
+  // No distribution: nothing above -infinity, or an infinite logit.
+  r.s = fabsf(p.top) < INFINITY ? fmaf(x.corr, p.w, p.s) : nan_f();
+  r.log_s = logf(r.s);
+  r.h = r.log_s - p.w / r.s * kLn2;
+  return r;
+}
+
+// The logit of a row's token (one thread); it may be overwritten once the block's gradients are.
+template <typename T>
+__device__ __forceinline__ float token_logit(const ScoresArgs& a, const Row& w, int r) {
+  const int t = a.logp != nullptr ? a.tokens[r] : -1;
+  return t >= 0 && t < w.V ? load1(elem_at<T>(w, t)) : 0.f;
+}
+
+// One thread: everything of a row but its alternatives and gradient.
+__device__ __forceinline__ void write_scores(const ScoresArgs& a, int r, const RowScore& q, float l) {
+  if (a.logp != nullptr) {
+    const int t = a.tokens[r];
+    a.logp[r] = t < 0 ? 0.f : t >= a.x.V ? nan_f() : log_p(a.x.tau, l, q.top, q.log_s);
+  }
+  if (a.entropy != nullptr) a.entropy[r] = q.h;
+  if (a.stats != nullptr) {
+    float* st = a.stats + (int64_t)r * kStats;
+    st[0] = q.top;
+    st[1] = q.s;
+    st[2] = q.h;
+    st[3] = q.top / a.x.tau + q.log_s;
+  }
+}
+
+// Parts of rows, one block each: grid rows * chunks.
+template <typename T, int U>
+__global__ __launch_bounds__(kThreads, 6) void scores_part_kernel(ScoresArgs a, Split sp) {
+  __shared__ float red[3][kThreads / 64];
+  const int r = blockIdx.x / sp.chunks, slot0 = blockIdx.x % sp.chunks * sp.nu * kThreads;
+  const Row w = until(row_at<T>(a.x.logits, a.x.ld, r, a.x.V), slot0 + sp.nu * kThreads);
+  Tile<kThreads, U> x;
+  load_tile<T>(x, w, slot0);
+  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{});
+  if (a.m > 0) tile_groups<T>(x, w, sp.glog, sp.gm + (int64_t)r * sp.gstride);
+  const Part p = block_part<kThreads>(a.x, mine, red);
+  if (threadIdx.x == 0) sp.parts[blockIdx.x] = make_float4(p.top, p.s, p.w, 0.f);
+}
+
+// A row's parts as one (a block of kThreads threads).
+__device__ __forceinline__ Part merge_parts(const VocabRows& x, const float4* parts, int n, float (*red)[kThreads / 64]) {
+  Part p{-INFINITY, 0.f, 0.f};
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const float4 q = parts[i];
+    const float top = fmaxf(p.top, q.x);
+    const Part b = rebased(x, Part{q.x, q.y, q.z}, top);
+    p = rebased(x, p, top);
+    p.s += b.s;
+    p.w += b.w;
+  }
+  return block_part<kThreads>(x, p, red);
+}
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kThreads) void scores_finish_kernel(ScoresArgs a, Split sp) {
+  __shared__ float red[3][kThreads / 64];
+  const int r = blockIdx.x;
+  const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
+  const RowScore q = row_score(a.x, merge_parts(a.x, sp.parts + (int64_t)r * sp.chunks, sp.chunks, red));
+  if (threadIdx.x == 0) write_scores(a, r, q, token_logit<T>(a, w, r));
+  if constexpr (TOP) {
+    __shared__ TopShared sh;
+    top_select<T>(w, sp.gm + (int64_t)r * sp.gstride, (w.slots + (1 << sp.glog) - 1) >> sp.glog, sp.glog, a.m,
+                  a.x.tau, q.top, q.log_s, a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh);
+  }
+}
+
+// Rows of one tile with alternatives, one block each.
+template <typename T, int U>
+__global__ __launch_bounds__(kThreads, 4) void scores_row_kernel(ScoresArgs a, int glog) {
+  __shared__ float red[3][kThreads / 64];
+  __shared__ float gm[U * kThreads];
+  __shared__ TopShared sh;
+  const int r = blockIdx.x;
+  const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
+  Tile<kThreads, U> x;
+  load_tile<T>(x, w, 0);
+  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{});
+  tile_groups<T>(x, w, glog, gm);
+  const Part p = block_part<kThreads>(a.x, mine, red);
+  const RowScore q = row_score(a.x, p);
+  if (threadIdx.x == 0) write_scores(a, r, q, token_logit<T>(a, w, r));
+  top_select<T>(w, gm, (w.slots + (1 << glog) - 1) >> glog, glog, a.m, a.x.tau, q.top, q.log_s,
+                a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh);
+}
+
+// What a logit's gradient is made of.
+struct ScoreGrad {
+  bool zero;          // a row without weight
+  int token;
+  float gl, ge;       // incoming gradients / tau
+  float top, inv, b;  // p = inv 2^d, log p + H = d ln 2 + b
+};
+
+__device__ __forceinline__ ScoreGrad score_grad(const VocabRows& x, const int32_t* tokens, const RowGrad& g, int r,
+                                                float top, float s, float h) {
+  ScoreGrad q;
+  q.token = tokens != nullptr ? tokens[r] : -1;
+  q.gl = g.g != nullptr && q.token >= 0 ? g.g[r] : 0.f;
+  q.ge = g.g_entropy != nullptr ? g.g_entropy[r] : 0.f;
+  q.zero = q.gl == 0.f && q.ge == 0.f;
+  if (q.token >= x.V && q.gl != 0.f) q.gl = nan_f();
+  const float it = 1.f / x.tau;
+  q.gl *= it;
+  q.ge *= it;
+  q.top = top;
+  q.inv = 1.f / s;
+  q.b = h - logf(s);
+  return q;
+}
+
+template <typename T>
+__device__ __forceinline__ void scores_grad_slot(const VocabRows& a, const ScoreGrad& q, const Row& w,
+                                                 const u32x4& x, int s, float (&v)[kE<T>]) {
+  const int t = q.token + w.o - s * kE<T>;  // the token's place in the slot
+  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+    const float d = scaled_floor(a, get<T>(x, c), q.top), p = exp2_fast(d) * q.inv;
+    v[c] = -p * fmaf(q.ge, fmaf(d, kLn2, q.b), q.gl);
+    if (c == t) v[c] += q.gl;
+  });
+}
+
+template <typename T, int U>
+__global__ __launch_bounds__(kThreads) void scores_grad_kernel(VocabRows x, const int32_t* tokens, const float* stats,
+                                                               RowGrad g, Split sp) {
+  const int r = blockIdx.x / sp.chunks, slot0 = blockIdx.x % sp.chunks * sp.nu * kThreads;
+  const Row w = until(row_at<T>(x.logits, x.ld, r, x.V), slot0 + sp.nu * kThreads), out = row_at<T>(g.dlogits, g.ldd, r, x.V);
+  const float* st = stats + (int64_t)r * kStats;
+  const ScoreGrad q = score_grad(x, tokens, g, r, st[0], st[1], st[2]);
+  if (q.zero) return zero_tile<T, kThreads>(w, out, slot0);
+  Tile<kThreads, U> l;
+  load_tile<T>(l, w, slot0);
+  load_last<T>(l, w);
+  each_slot(l, [&](const u32x4& s, int u) __attribute__((always_inline)) {
+    if (l.slot(u) >= w.slots) return;
+    float v[kE<T>];
+    scores_grad_slot<T>(x, q, w, s, l.slot(u), v);
+    store_slot<T>(w, out, l.slot(u), v);
+  });
+}
+
+// Whole rows without alternatives, one block each, and their gradient where one is asked for.
+template <typename T, int NTH, int U>
+__global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void scores_whole_kernel(ScoresArgs a, RowGrad g) {
+  __shared__ float red[3][NTH / 64];
+  __shared__ float token;
+  const int r = blockIdx.x;
+  const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
+  Tile<NTH, U> x;
+  load_tile<T>(x, w, 0);
+  if (threadIdx.x == 0) token = token_logit<T>(a, w, r);
+  const Part p = block_part<NTH>(a.x, tile_sums<T, false>(a.x, x, w, NoFix{}), red);
+  const RowScore q = row_score(a.x, p);
+  if (threadIdx.x == 0) write_scores(a, r, q, token);
+  if (g.dlogits == nullptr) return;
+  const Row out = row_at<T>(g.dlogits, g.ldd, r, a.x.V);
+  const ScoreGrad d = score_grad(a.x, a.tokens, g, r, q.top, q.s, q.h);
+  if (d.zero) return zero_tile<T, NTH>(w, out, 0);
+  each_slot(x, [&](const u32x4& s, int u) __attribute__((always_inline)) {
+    if (x.slot(u) >= w.slots) return;
+    float v[kE<T>];
+    scores_grad_slot<T>(a.x, d, w, s, x.slot(u), v);
+    store_slot<T>(w, out, x.slot(u), v);
+  });
+}
+
+template <typename T>
+hipError_t scores_grad(const VocabRows& x, const int32_t* tokens, const float* stats, const RowGrad& g,
+                       hipStream_t s) {
+  const Split sp = split_of<T>(x, 0, nullptr);
+  by_u(sp.nu, [&](auto u) {
+    hipLaunchKernelGGL((scores_grad_kernel<T, u.value>), dim3((unsigned)x.rows * sp.chunks), dim3(kThreads), 0, s, x,
+                       tokens, stats, g, sp);
+  });
+  return note_hip(hipGetLastError());
+}
+
+template <typename T>
+hipError_t scores(const ScoresArgs& a, const RowGrad& g, void* ws, hipStream_t s) {
+  const int slots = slots_most<T>(a.x);
+  const dim3 rows(a.x.rows);
+  if (a.m > 0 && slots <= kTileU * kThreads) {
+    by_u((slots + kThreads - 1) / kThreads, [&](auto u) {
+      hipLaunchKernelGGL((scores_row_kernel<T, u.value>), rows, dim3(kThreads), 0, s, a, group_log(slots));
+    });
+    return note_hip(hipGetLastError());
+  }
+  if (a.m == 0 && (slots <= kTileU * kThreads || (g.dlogits != nullptr && whole_row(a.x.rows, slots)))) {
+    by_whole(slots, [&](auto k) {
+      hipLaunchKernelGGL((scores_whole_kernel<T, k.kNth, k.kU>), rows, dim3(k.kNth), 0, s, a, g);
+    });
+    return note_hip(hipGetLastError());
+  }
+  const Split sp = split_of<T>(a.x, a.m, ws);
+  by_u(sp.nu, [&](auto u) {
+    hipLaunchKernelGGL((scores_part_kernel<T, u.value>), dim3((unsigned)a.x.rows * sp.chunks), dim3(kThreads), 0, s,
+                       a, sp);
+  });
+  if (a.m > 0)
+    hipLaunchKernelGGL((scores_finish_kernel<T, true>), rows, dim3(kThreads), 0, s, a, sp);
+  else
+    hipLaunchKernelGGL((scores_finish_kernel<T, false>), rows, dim3(kThreads), 0, s, a, sp);
+  const hipError_t e = note_hip(hipGetLastError());
+  return e != hipSuccess || g.dlogits == nullptr ? e : scores_grad<T>(a.x, a.tokens, a.stats, g, s);
+}
+
+}  // namespace
+
+size_t scores_bytes(int rows, int V, int m) {
+  size_t most = 0;
+  // Either type, rows at any element or at whole slots; never fewer bytes for more rows.
+  const auto add = [&](int slots) {
+    const size_t slabs = (slots + kThreads - 1) / kThreads, coarse = (slabs + kTileU - 1) / kTileU;
+    size_t b = std::max(rows * coarse, std::min<size_t>(rows * slabs, kBlocks + rows)) * sizeof(float4);
+    if (m > 0) b += (size_t)rows * ((slots >> group_log(slots)) + 1) * 4;
+    most = std::max(most, b);
+  };
+  add((V + kE<float> - 1) / kE<float>);
+  add((V + kE<uint16_t> - 1) / kE<uint16_t>);
+  add(slots_most<float>(V));
+  add(slots_most<uint16_t>(V));
+  return most;
+}
+
+hipError_t launch_scores(const ScoresArgs& a, const RowGrad& g, void* ws, hipStream_t s) {
+  return a.x.bf16 ? scores<uint16_t>(a, g, ws, s) : scores<float>(a, g, ws, s);
+}
+hipError_t launch_scores_grad(const VocabRows& x, const int32_t* tokens, const float* stats, const RowGrad& g,
+                              hipStream_t s) {
+  return x.bf16 ? scores_grad<uint16_t>(x, tokens, stats, g, s) : scores_grad<float>(x, tokens, stats, g, s);
+}
+
+}  // namespace de
