@@ -74,12 +74,14 @@ __device__ __forceinline__ u32x4 all_dropped() {
   const uint32_t v = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
   return u32x4{v, v, v, v};
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <typename T>
 __device__ __forceinline__ u32x4 packed(const float (&v)[kE<T>]) {
   u32x4 x;
   each<4>([&](auto c) __attribute__((always_inline)) {
     if constexpr (sizeof(T) == 4) x[c.value] = __float_as_uint(v[c]);
-    else x[c.value] = bf16_bits(v[2 * c]) | bf16_bits(v[2 * c + 1]) << 16;
+    else x[c.value] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * c], v[2 * c + 1]}), bf16x2));
   });
   return x;
 }
@@ -153,21 +155,24 @@ struct Tile {
   __device__ __forceinline__ int slot(int u) const { return slot0 + u * NTH + threadIdx.x; }
 };
 
+// Every thread loads U slots, without a branch, so that the wait for one does not wait for
+// those after it; a slot that is not a whole one of the row is read at the nearest that is
+// and replaced when it is taken (tile_sums) or not stored.
 template <typename T, int NTH, int U>
 __device__ __forceinline__ void load_tile(Tile<NTH, U>& x, const Row& w, int slot0) {
   x.slot0 = slot0;
   x.ragged = w.f1 < w.slots && w.slots > slot0;
   x.m = (w.slots - slot0 + NTH - 1) / NTH - x.ragged;
-  if (x.m > 0 && slot0 < w.f0) x.x[0] = load_edge<T>(w, x.slot(0));
-  each<U>([&](auto u) __attribute__((always_inline)) {
-    if (u >= x.m || (u == 0 && slot0 < w.f0)) return;
-    if (slot0 + (u + 1) * NTH <= w.f1) {
-      x.x[u] = load_stream16(w.base + (int64_t)(slot0 + u * NTH) * 16 + threadIdx.x * 16);
-    } else {
-      x.x[u] = all_dropped<T>();
-      if (x.slot(u) < w.f1) x.x[u] = load_stream16(w.base + (int64_t)x.slot(u) * 16);
-    }
-  });
+  if (w.f0 < w.f1)
+    each<U>([&](auto u) __attribute__((always_inline)) {
+      x.x[u] = load_stream16(w.base + (uint32_t)min(max(x.slot(u), w.f0), w.f1 - 1) * 16u);
+    });
+  if (x.m > 0 && slot0 < w.f0) {
+    x.x[0] = load_edge<T>(w, x.slot(0));
+    // Waited for here: a load that only some rows have in flight would make all of them wait
+    // for everything at their first slot.
+    asm volatile("" : "+v"(x.x[0]));
+  }
 }
 template <typename T, int NTH, int U>
 __device__ __forceinline__ void load_last(Tile<NTH, U>& x, const Row& w) {
@@ -331,6 +336,7 @@ __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, c
     float top = p.top;
     each<k>([&](auto i) __attribute__((always_inline)) {
       if (u0 + i >= x.m) return;
+      if (x.slot0 + (u0 + i + 1) * NTH > w.f1 && x.slot(u0 + i) >= w.slots) x.x[u0 + i] = all_dropped<T>();
       fix(x.x[u0 + i], u0 + i);
       rise(top, x.x[u0 + i]);
     });
@@ -406,8 +412,10 @@ __device__ __forceinline__ void drop_marked(u32x4& x, int u, const Marks<T, NTH,
   if (!(__builtin_amdgcn_readfirstlane(k.slots[wave][u >> 5]) >> (u & 31) & 1)) return;
   const int i = (u * NTH + threadIdx.x) * kE<T>;
   const uint32_t b = k.bits[i >> 5] >> (i & 31);
-  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
-    if (b >> c & 1) drop<T>(x, c);
+  const auto all = [&](int at) { return (uint32_t)((int32_t)(b << (31 - at)) >> 31); };  // a bit in every place
+  each<4>([&](auto c) __attribute__((always_inline)) {
+    const uint32_t mask = sizeof(T) == 4 ? all(c) : (all(2 * c) & 0xffffu) | all(2 * c + 1) << 16;
+    x[c.value] = (x[c.value] & ~mask) | (all_dropped<T>()[0] & mask);
   });
 }
 
@@ -473,10 +481,11 @@ inline void by_whole(int slots, const F& f) {
   else if (slots <= 256 * 16) f(Whole<256, 16>{});
   else if (slots <= 512 * 16) f(Whole<512, 16>{});
   else if (slots <= 512 * 20) f(Whole<512, 20>{});
+  else if (slots <= 512 * 25) f(Whole<512, 25>{});
   else f(Whole<512, 50>{});
 }
 // Waves of a SIMD that a block's registers leave room for.
-constexpr int whole_waves(int nth, int u) { return u <= 20 ? 4 : nth / 256; }
+constexpr int whole_waves(int nth, int u) { return u <= 25 ? 4 : nth / 256; }
 
 inline bool whole_row(int rows, int slots) {
   return slots <= kWholeSlots && (slots <= kTileU * kThreads || rows >= 128);

@@ -309,6 +309,7 @@ struct ScoreGrad {
   int token;
   float gl, ge;       // incoming gradients / tau
   float top, inv, b;  // p = inv 2^d, log p + H = d ln 2 + b
+  float k;            // -gl inv
 };
 
 __device__ __forceinline__ ScoreGrad score_grad(const VocabRows& x, const int32_t* tokens, const RowGrad& g, int r,
@@ -325,17 +326,27 @@ __device__ __forceinline__ ScoreGrad score_grad(const VocabRows& x, const int32_
   q.top = top;
   q.inv = 1.f / s;
   q.b = h - logf(s);
+  q.k = -q.gl * q.inv;
   return q;
 }
 
-template <typename T>
-__device__ __forceinline__ void scores_grad_slot(const VocabRows& a, const ScoreGrad& q, const Row& w,
-                                                 const u32x4& x, int s, float (&v)[kE<T>]) {
-  const int t = q.token + w.o - s * kE<T>;  // the token's place in the slot
-  each<kE<T>>([&](auto c) __attribute__((always_inline)) {
-    const float d = scaled_floor(a, get<T>(x, c), q.top), p = exp2_fast(d) * q.inv;
-    v[c] = -p * fmaf(q.ge, fmaf(d, kLn2, q.b), q.gl);
-    if (c == t) v[c] += q.gl;
+// A tile's gradients.  `entropy`: with its part.
+template <typename T, bool entropy, int NTH, int U>
+__device__ __forceinline__ void scores_grad_tile(const VocabRows& a, const ScoreGrad& q, Tile<NTH, U>& x, const Row& w,
+                                                 const Row& out) {
+  each_slot(x, [&](const u32x4& l, int u) __attribute__((always_inline)) {
+    const int s = x.slot(u);
+    if (s >= w.slots) return;
+    float v[kE<T>];
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+      const float d = scaled_floor(a, get<T>(l, c), q.top), e = exp2_fast(d);
+      if constexpr (entropy) v[c] = -e * q.inv * fmaf(q.ge, fmaf(d, kLn2, q.b), q.gl);
+      else v[c] = e * q.k;
+    });
+    const int t = q.token + w.o - s * kE<T>;  // the token's place in the slot
+    if (t >= 0 && t < kE<T>)
+      each<kE<T>>([&](auto c) __attribute__((always_inline)) { v[c] += t == c ? q.gl : 0.f; });
+    store_slot<T>(w, out, s, v);
   });
 }
 
@@ -350,12 +361,8 @@ __global__ __launch_bounds__(kThreads) void scores_grad_kernel(VocabRows x, cons
   Tile<kThreads, U> l;
   load_tile<T>(l, w, slot0);
   load_last<T>(l, w);
-  each_slot(l, [&](const u32x4& s, int u) __attribute__((always_inline)) {
-    if (l.slot(u) >= w.slots) return;
-    float v[kE<T>];
-    scores_grad_slot<T>(x, q, w, s, l.slot(u), v);
-    store_slot<T>(w, out, l.slot(u), v);
-  });
+  if (q.ge == 0.f) scores_grad_tile<T, false>(x, q, l, w, out);
+  else scores_grad_tile<T, true>(x, q, l, w, out);
 }
 
 // Whole rows without alternatives, one block each, and their gradient where one is asked for.
@@ -375,12 +382,8 @@ __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void scores_whole_kernel(
   const Row out = row_at<T>(g.dlogits, g.ldd, r, a.x.V);
   const ScoreGrad d = score_grad(a.x, a.tokens, g, r, q.top, q.s, q.h);
   if (d.zero) return zero_tile<T, NTH>(w, out, 0);
-  each_slot(x, [&](const u32x4& s, int u) __attribute__((always_inline)) {
-    if (x.slot(u) >= w.slots) return;
-    float v[kE<T>];
-    scores_grad_slot<T>(a.x, d, w, s, x.slot(u), v);
-    store_slot<T>(w, out, x.slot(u), v);
-  });
+  if (d.ge == 0.f) scores_grad_tile<T, false>(a.x, d, x, w, out);
+  else scores_grad_tile<T, true>(a.x, d, x, w, out);
 }
 
 template <typename T>

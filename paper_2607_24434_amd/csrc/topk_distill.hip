@@ -9,7 +9,7 @@ namespace {
 // A teacher's list as one wave takes it, in 64 bits: the loss is a small difference of its
 // terms.  Two slots a lane.
 struct List {
-  int32_t id[kTopMax];     // -1: no entry
+  alignas(16) int32_t id[kTopMax];  // -1: no entry
   int32_t first[kTopMax];  // the first slot of the same id; an entry's own is itself
   double e[kTopMax];       // exp((l - em) / tau)
   double p[kTopMax];       // the teacher's probability (0 but in an entry's first slot)
@@ -45,11 +45,16 @@ __device__ __forceinline__ void take_list(const DistillArgs& a, const Row& w, in
     val[k] = ids[k] >= 0 ? (double)a.values[(int64_t)r * a.m + j] : -INFINITY;
   }
   wave_sync();
-  for (int i = a.m - 1; i >= 0; --i) {
-    const int id = q.id[i];
+  for (int i = (a.m - 1) / 4 * 4; i >= 0; i -= 4) {
+    const int4 id = *reinterpret_cast<const int4*>(&q.id[i]);
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (id == ids[k] && i < lane + 64 * k) first[k] = i;
+    for (int k = 0; k < 2; ++k) {
+      const int j = lane + 64 * k;
+      if (id.w == ids[k] && i + 3 < j) first[k] = i + 3;
+      if (id.z == ids[k] && i + 2 < j) first[k] = i + 2;
+      if (id.y == ids[k] && i + 1 < j) first[k] = i + 1;
+      if (id.x == ids[k] && i < j) first[k] = i;
+    }
   }
   bool own[2];
 #pragma unroll
