@@ -63,6 +63,14 @@ __device__ __forceinline__ float get(const u32x4& x, int c) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(x[c]);
   else return c & 1 ? bf16_hi(x[c >> 1]) : bf16_lo(x[c >> 1]);
 }
+// ... for any c, without an array in memory.
+template <typename T>
+__device__ __forceinline__ float get_at(const u32x4& x, int c) {
+  const int d = sizeof(T) == 4 ? c : c >> 1;
+  const uint32_t lo = d & 1 ? x[1] : x[0], hi = d & 1 ? x[3] : x[2], v = d & 2 ? hi : lo;
+  if constexpr (sizeof(T) == 4) return __uint_as_float(v);
+  else return c & 1 ? bf16_hi(v) : bf16_lo(v);
+}
 // -infinity in its place.
 template <typename T>
 __device__ __forceinline__ void drop(u32x4& x, int c) {
@@ -234,6 +242,10 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 // ... and the lower index first.
 __device__ __forceinline__ uint64_t order_key(float v, int i) {
   return (uint64_t)order_key(v) << 32 | (0xffffffffu - (uint32_t)i);
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t b = (uint32_t)(k >> 32);
+  return __uint_as_float(b ^ (b >> 31 ? 0x80000000u : 0xffffffffu));
 }
 __device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
 

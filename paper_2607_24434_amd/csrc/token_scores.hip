@@ -18,9 +18,9 @@ constexpr int kBatch = 8;               // slots a thread loads at once
 
 struct TopShared {
   uint64_t groups[kGroupCap];
-  uint64_t list[kListCap];
+  alignas(16) uint64_t list[kListCap];
   uint64_t bound;
-  int ngroups, n, need, through;
+  int ngroups, n, through;
   int red[2][kThreads / 64];
 };
 
@@ -65,19 +65,31 @@ __device__ __attribute__((noinline)) uint64_t prune(uint64_t* list, int& n_share
 }
 
 // The best m of a row in descending order, ties to the lower index, from its groups' maxima
-// gm[0, G) (a block of kThreads threads).
+// gm[0, G) (a block of kThreads threads).  `side` is run by the second wave's first thread while
+// the first wave is busy alone.
 //   1. Each thread's best group; a bound that m to m + kSlack of the threads reach, by
 //      bisection in one wave.  At least m groups are at or over it.
 //   2. Those groups' logits at or over the bound's value go to a list; both lists are
 //      pruned to their best m whenever they could overflow (rows of many equal or sorted
 //      logits).
 //   3. Each logit's rank in the list is its place.
-template <typename T>
+template <typename T, typename F>
 __device__ void top_select(const Row& w, const float* gm, int G, int glog, int m, float tau, float top,
-                           float log_s, int32_t* idx, float* logp, TopShared& sh) {
+                           float log_s, int32_t* idx, float* logp, TopShared& sh, const F& side) {
   const int tid = threadIdx.x;
+  // The first kBatch groups of a thread stay in registers.
+  float v0[kBatch];
+  each<kBatch>([&](auto i) __attribute__((always_inline)) {
+    const int g = i * kThreads + tid;
+    v0[i] = g < G ? gm[g] : 0.f;
+  });
+  const auto group_key = [&](float v, int g) { return g < G ? order_key(v, g) : 0; };
   uint64_t best = 0;
-  for (int g = tid; g < G; g += kThreads) {
+  each<kBatch>([&](auto i) __attribute__((always_inline)) {
+    const uint64_t k = group_key(v0[i], i * kThreads + tid);
+    best = k > best ? k : best;
+  });
+  for (int g = kBatch * kThreads + tid; g < G; g += kThreads) {
     const uint64_t k = order_key(gm[g], g);
     best = k > best ? k : best;
   }
@@ -85,110 +97,132 @@ __device__ void top_select(const Row& w, const float* gm, int G, int glog, int m
   if (tid == 0) sh.ngroups = sh.n = 0;
   __syncthreads();
   if (tid < kWave) {
-    uint64_t v[kThreads / kWave];
+    constexpr int Q = kThreads / kWave;
+    uint64_t v[Q];
+    uint32_t h[Q], all = 0, any = ~0u;
 #pragma unroll
-    for (int i = 0; i < kThreads / kWave; ++i) v[i] = sh.list[i * kWave + tid];
-    const auto count = [&](uint64_t b) {
+    for (int i = 0; i < Q; ++i) {
+      v[i] = sh.list[i * kWave + tid];
+      h[i] = (uint32_t)(v[i] >> 32);
+      all |= h[i];
+      any &= h[i];
+    }
+    // The bits in which the values differ at all.
+    for (int o = 32; o > 0; o >>= 1) {
+      all |= __shfl_xor(all, o, kWave);
+      any &= __shfl_xor(any, o, kWave);
+    }
+    const auto count = [&](auto ge) __attribute__((always_inline)) {
       int c = 0;
 #pragma unroll
-      for (int i = 0; i < kThreads / kWave; ++i) c += __popcll(__ballot(v[i] >= b));
+      for (int i = 0; i < Q; ++i) c += __popcll(__ballot(ge(i)));
       return c;
     };
-    uint64_t lo = 1;
-    int c = count(lo);
+    uint32_t lo = any, differ = __builtin_amdgcn_readfirstlane(all ^ any);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    int c = count([&](int i) { return v[i] != 0; });
+    uint64_t bound = 1;
     if (c > m + kSlack) {
-      lo = 0;
-      for (int b = 63; b >= 0; --b) {
-        const uint64_t mid = lo | 1ull << b;
-        const int k = count(mid);
+      // The largest value with m or more at or over it, or the first with few enough.
+      c = kThreads;
+      while (differ != 0 && c > m + kSlack) {
+        const uint32_t bit = 0x80000000u >> __builtin_clz(differ), mid = lo | bit;
+        differ &= bit - 1;
+        const int k = count([&](int i) { return h[i] >= mid; });
         if (k < m) continue;
         lo = mid;
         c = k;
-        if (k <= m + kSlack) break;
+      }
+      bound = (uint64_t)lo << 32;
+      // Equal values: the lower indices.
+      for (uint32_t bit = 0x80000000u; bit != 0 && c > m + kSlack; bit >>= 1) {
+        const uint64_t mid = bound | bit;
+        const int k = count([&](int i) { return v[i] >= mid; });
+        if (k < m) continue;
+        bound = mid;
+        c = k;
       }
     }
     if (tid == 0) {
-      sh.bound = lo;
+      sh.bound = bound;
       sh.through = c;
     }
   }
+  if (tid == kWave) side();
   __syncthreads();
   uint64_t bound = sh.bound;
   const int rounds = (G + kThreads - 1) / kThreads;
-  const bool fits = (int64_t)sh.through * rounds <= kGroupCap;
-  for (int i = 0; i < rounds; ++i) {
-    if (!fits) {
+  if (rounds <= kBatch && sh.through * rounds <= kGroupCap) {
+    each<kBatch>([&](auto i) __attribute__((always_inline)) {
+      const uint64_t k = group_key(v0[i], i * kThreads + tid);
+      if (k >= bound) sh.groups[atomicAdd(&sh.ngroups, 1)] = k;
+    });
+  } else {
+    for (int i = 0; i < rounds; ++i) {
       __syncthreads();
       const bool full = sh.ngroups + kThreads > kGroupCap;
       __syncthreads();  // every thread has read it before one appends
       if (full) bound = prune<kGroupCap>(sh.groups, sh.ngroups, m, sh);
+      const int g = i * kThreads + tid;
+      const uint64_t k = g < G ? order_key(gm[g], g) : 0;
+      if (k >= bound) sh.groups[atomicAdd(&sh.ngroups, 1)] = k;
     }
-    const int g = i * kThreads + tid;
-    const uint64_t k = g < G ? order_key(gm[g], g) : 0;
-    if (k >= bound) sh.groups[atomicAdd(&sh.ngroups, 1)] = k;
   }
   __syncthreads();
   const int work = sh.ngroups << glog;
   // A logit of the bound's value may beat the bound's group: only its value counts.
   bound = bound >> 32 << 32;
+  const auto first_of = [&](int j) {  // the row's element that slot j of the work starts at
+    return ((key_index(sh.groups[j >> glog]) << glog) + (j & ((1 << glog) - 1))) * kE<T> - w.o;
+  };
   for (int j0 = 0; j0 < work; j0 += kBatch * kThreads) {
+    const int n0 = sh.n;
+    __syncthreads();  // every thread has read it before one appends
     u32x4 x[kBatch];
     int first[kBatch];
     each<kBatch>([&](auto b) __attribute__((always_inline)) {
       const int j = j0 + b * kThreads + tid;
       x[b] = all_dropped<T>();
-      first[b] = INT32_MIN / 2;
+      first[b] = w.V;
       if (j < work) {
-        const int s = (key_index(sh.groups[j >> glog]) << glog) + (j & ((1 << glog) - 1));
-        if (s < w.slots) {
-          x[b] = load_edge<T>(w, s);
-          first[b] = s * kE<T> - w.o;
-        }
+        first[b] = first_of(j);
+        if (first[b] < w.V) x[b] = load_edge<T>(w, (first[b] + w.o) / kE<T>);
       }
     });
-    // A bit for each logit at or over the bound.
-    uint32_t take[kBatch];
-    int mine = 0;
     each<kBatch>([&](auto b) __attribute__((always_inline)) {
-      take[b] = 0;
-      each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+      if (j0 + b * kThreads >= work) return;
+      float most = -INFINITY;
+      each<kE<T>>([&](auto c) __attribute__((always_inline)) { most = fmaxf(most, get<T>(x[b], c)); });
+      if ((uint64_t)order_key(most) << 32 < (bound >> 32 << 32)) return;
+#pragma unroll 1
+      for (int c = 0; c < kE<T>; ++c) {
+        const float v = get_at<T>(x[b], c);
         const int i = first[b] + c;
-        if (i >= 0 && i < w.V && order_key(get<T>(x[b], c), i) >= bound) take[b] |= 1u << c;
-      });
-      mine += __popc(take[b]);
+        const uint64_t k = order_key(v, i);
+        if (i < 0 || i >= w.V || k < bound) continue;
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < kListCap) sh.list[at] = k;
+      }
     });
-    if (tid == 0) sh.need = 0;
     __syncthreads();
-    if (mine) atomicAdd(&sh.need, mine);
+    if (sh.n <= kListCap) continue;
+    // No room: what these slots added goes, and they are taken again, one logit of each at
+    // a time.
     __syncthreads();
-    const bool room = sh.n + sh.need <= kListCap;
-    __syncthreads();
-    if (room) {
-      int at = mine ? atomicAdd(&sh.n, mine) : 0;
-      each<kBatch>([&](auto b) __attribute__((always_inline)) {
-        if (take[b] == 0) return;
-        each<kE<T>>([&](auto c) __attribute__((always_inline)) {
-          if (take[b] >> c & 1) sh.list[at++] = order_key(get<T>(x[b], c), first[b] + c);
-        });
-      });
-    } else {
-      // One logit a thread at a time, read again.
+    if (tid == 0) sh.n = n0;
 #pragma unroll 1
-      for (int b = 0; b < kBatch; ++b)
+    for (int b = 0; b < kBatch; ++b)
 #pragma unroll 1
-        for (int c = 0; c < kE<T>; ++c) {
-          __syncthreads();
-          const bool full = sh.n + kThreads > kListCap;
-          __syncthreads();  // every thread has read it before one appends
-          if (full) bound = prune<kListCap>(sh.list, sh.n, m, sh);
-          const int j = j0 + b * kThreads + tid;
-          if (j >= work) continue;
-          const int i = ((key_index(sh.groups[j >> glog]) << glog) + (j & ((1 << glog) - 1))) * kE<T> - w.o + c;
-          if (i < 0 || i >= w.V) continue;
-          const uint64_t k = order_key(load1(elem_at<T>(w, i)), i);
-          if (k >= bound) sh.list[atomicAdd(&sh.n, 1)] = k;
-        }
-    }
+      for (int c = 0; c < kE<T>; ++c) {
+        __syncthreads();
+        const bool full = sh.n + kThreads > kListCap;
+        __syncthreads();
+        if (full) bound = prune<kListCap>(sh.list, sh.n, m, sh);
+        const int j = j0 + b * kThreads + tid, i = j < work ? first_of(j) + c : -1;
+        if (i < 0 || i >= w.V) continue;
+        const uint64_t k = order_key(load1(elem_at<T>(w, i)), i);
+        if (k >= bound) sh.list[atomicAdd(&sh.n, 1)] = k;
+      }
     __syncthreads();
   }
   if (sh.n > kThreads) prune<kListCap>(sh.list, sh.n, m, sh);
@@ -196,11 +230,15 @@ __device__ void top_select(const Row& w, const float* gm, int G, int glog, int m
   if (tid >= n) return;
   const uint64_t mine = sh.list[tid];
   int rank = 0;
-  for (int i = 0; i < n; ++i) rank += sh.list[i] > mine;
+#pragma unroll 4
+  for (int i = 0; i + 1 < n; i += 2) {
+    const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(&sh.list[i]);
+    rank += (k.x > mine) + (k.y > mine);
+  }
+  if (n & 1) rank += sh.list[n - 1] > mine;
   if (rank >= m) return;
-  const int i = key_index(mine);
-  idx[rank] = i;
-  logp[rank] = log_p(tau, load1(elem_at<T>(w, i)), top, log_s);
+  idx[rank] = key_index(mine);
+  logp[rank] = log_p(tau, key_value(mine), top, log_s);
 }
 
 // ---------------------------------------------------------------- token scores
@@ -275,12 +313,15 @@ __global__ __launch_bounds__(kThreads) void scores_finish_kernel(ScoresArgs a, S
   __shared__ float red[3][kThreads / 64];
   const int r = blockIdx.x;
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
+  const float token = threadIdx.x == kWave ? token_logit<T>(a, w, r) : 0.f;
   const RowScore q = row_score(a.x, merge_parts(a.x, sp.parts + (int64_t)r * sp.chunks, sp.chunks, red));
-  if (threadIdx.x == 0) write_scores(a, r, q, token_logit<T>(a, w, r));
-  if constexpr (TOP) {
+  const auto rest = [&] { write_scores(a, r, q, token); };
+  if constexpr (!TOP) {
+    if (threadIdx.x == kWave) rest();
+  } else {
     __shared__ TopShared sh;
     top_select<T>(w, sp.gm + (int64_t)r * sp.gstride, (w.slots + (1 << sp.glog) - 1) >> sp.glog, sp.glog, a.m,
-                  a.x.tau, q.top, q.log_s, a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh);
+                  a.x.tau, q.top, q.log_s, a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh, rest);
   }
 }
 
@@ -294,13 +335,13 @@ __global__ __launch_bounds__(kThreads, 4) void scores_row_kernel(ScoresArgs a, i
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
   Tile<kThreads, U> x;
   load_tile<T>(x, w, 0);
+  const float token = threadIdx.x == kWave ? token_logit<T>(a, w, r) : 0.f;
   const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{});
   tile_groups<T>(x, w, glog, gm);
   const Part p = block_part<kThreads>(a.x, mine, red);
   const RowScore q = row_score(a.x, p);
-  if (threadIdx.x == 0) write_scores(a, r, q, token_logit<T>(a, w, r));
   top_select<T>(w, gm, (w.slots + (1 << glog) - 1) >> glog, glog, a.m, a.x.tau, q.top, q.log_s,
-                a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh);
+                a.top_idx + (int64_t)r * a.m, a.top_logp + (int64_t)r * a.m, sh, [&] { write_scores(a, r, q, token); });
 }
 
 // What a logit's gradient is made of.
