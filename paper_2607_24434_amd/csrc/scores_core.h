@@ -294,16 +294,27 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return t;
 }
 
-template <typename Op>
-__device__ __forceinline__ double wave_all(double v, Op op) {
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, kWave));
-  return v;
+template <int ctrl, int rows>
+__device__ __forceinline__ double dpp_add(double v) {  // lanes that take nothing add 0
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, ctrl, rows, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), ctrl, rows, 0xF, false);
+  return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double read_lane(double v, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ double wave_sum64(double v) {
-  return wave_all(v, [](double a, double b) { return a + b; });
-}
-__device__ __forceinline__ double wave_max64(double v) {
-  return wave_all(v, [](double a, double b) { return a > b ? a : b; });
+  v = dpp_add<0xB1, 0xF>(v);
+  v = dpp_add<0x4E, 0xF>(v);
+  v = dpp_add<0x141, 0xF>(v);
+  v = dpp_add<0x140, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);
+  v = dpp_add<0x143, 0xC>(v);
+  return read_lane(v, 63);
 }
 
 // ---------------------------------------------------------------- sums over a tile
@@ -483,8 +494,9 @@ template <int NTH, int U>
 struct Whole {
   static constexpr int kNth = NTH, kU = U;
 };
-// f with the smallest block that holds the slots.
-template <typename F>
+// f with the smallest block that holds the slots.  Pair: the most slots a thread with which a
+// CU's registers hold two blocks, so that one computes while the other loads.
+template <int Pair, typename F>
 inline void by_whole(int slots, const F& f) {
   if (slots <= 256) f(Whole<256, 1>{});
   else if (slots <= 256 * 2) f(Whole<256, 2>{});
@@ -492,12 +504,11 @@ inline void by_whole(int slots, const F& f) {
   else if (slots <= 256 * 8) f(Whole<256, 8>{});
   else if (slots <= 256 * 16) f(Whole<256, 16>{});
   else if (slots <= 512 * 16) f(Whole<512, 16>{});
-  else if (slots <= 512 * 20) f(Whole<512, 20>{});
-  else if (slots <= 512 * 25) f(Whole<512, 25>{});
+  else if (slots <= 512 * Pair) f(Whole<512, Pair>{});
   else f(Whole<512, 50>{});
 }
 // Waves of a SIMD that a block's registers leave room for.
-constexpr int whole_waves(int nth, int u) { return u <= 25 ? 4 : nth / 256; }
+constexpr int whole_waves(int nth, int u) { return u < 50 ? 4 : nth / 256; }
 
 inline bool whole_row(int rows, int slots) {
   return slots <= kWholeSlots && (slots <= kTileU * kThreads || rows >= 128);

@@ -449,7 +449,7 @@ hipError_t scores(const ScoresArgs& a, const RowGrad& g, void* ws, hipStream_t s
     return note_hip(hipGetLastError());
   }
   if (a.m == 0 && (slots <= kTileU * kThreads || (g.dlogits != nullptr && whole_row(a.x.rows, slots)))) {
-    by_whole(slots, [&](auto k) {
+    by_whole<25>(slots, [&](auto k) {
       hipLaunchKernelGGL((scores_whole_kernel<T, k.kNth, k.kU>), rows, dim3(k.kNth), 0, s, a, g);
     });
     return note_hip(hipGetLastError());

@@ -6,20 +6,19 @@ namespace {
 
 // ---------------------------------------------------------------- distillation
 
-// A teacher's list as one wave takes it, in 64 bits: the loss is a small difference of its
-// terms.  Two slots a lane.
+// A teacher's list, in 64 bits: the loss is a small difference of its terms.
 struct List {
   alignas(16) int32_t id[kTopMax];  // -1: no entry
+  float l[kTopMax];        // the student's logits, and
+  float val[kTopMax];      // the teacher's values of the entries
   int32_t first[kTopMax];  // the first slot of the same id; an entry's own is itself
   double e[kTopMax];       // exp((l - em) / tau)
-  double p[kTopMax];       // the teacher's probability (0 but in an entry's first slot)
-  double em, se;           // the entries' largest logit; sum e
-  double sp, pl;           // sum p; sum p (log p - (l - em) / tau)
-  double P;                // the teacher's mass outside the list
-  int none;                // no entry at all
+  double p[kTopMax];       // exp(value - vmax), later the probability (0 but in first slots)
+  float em, vmax;          // the entries' largest logit; the largest value (0 with tail)
   // Once the sum over the other logits is known:
   float own[kTopMax];      // an entry's gradient tau (q - p), in its first slot
   float k;                 // tau (Q - P) / (sum outside): the others' is k exp((l - top) / tau)
+  int none;                // no entry at all
 };
 
 __device__ __forceinline__ void wave_sync() {
@@ -27,101 +26,104 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// One wave: everything that does not need the other logits.
-template <typename T>
-__device__ __forceinline__ void take_list(const DistillArgs& a, const Row& w, int r, List& q) {
-  const int lane = threadIdx.x & 63;
-  const double tau = a.x.tau;
-  int ids[2], first[2];
-  double l[2], val[2];
+// What the list has in memory, before a gradient may be written over it (NTH threads).
+template <typename T, int NTH>
+__device__ __forceinline__ void fetch_list(const DistillArgs& a, const Row& w, int r, List& q) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int j = lane + 64 * k;
-    const int id = j < a.m ? a.ids[(int64_t)r * a.m + j] : -1;
-    ids[k] = id >= 0 && id < w.V ? id : -1;
-    first[k] = j;
-    q.id[j] = ids[k];
-    l[k] = ids[k] >= 0 ? (double)load1(elem_at<T>(w, id)) : -INFINITY;
-    val[k] = ids[k] >= 0 ? (double)a.values[(int64_t)r * a.m + j] : -INFINITY;
+  for (int j = threadIdx.x; j < kTopMax; j += NTH) {
+    const int at = j < a.m ? a.ids[(int64_t)r * a.m + j] : -1, id = at >= 0 && at < w.V ? at : -1;
+    const float val = j < a.m ? a.values[(int64_t)r * a.m + j] : 0.f;
+    q.id[j] = id;
+    q.l[j] = id >= 0 ? load1(elem_at<T>(w, id)) : -INFINITY;
+    q.val[j] = id >= 0 ? val : -INFINITY;
   }
-  wave_sync();
-  for (int i = (a.m - 1) / 4 * 4; i >= 0; i -= 4) {
-    const int4 id = *reinterpret_cast<const int4*>(&q.id[i]);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int j = lane + 64 * k;
-      if (id.w == ids[k] && i + 3 < j) first[k] = i + 3;
-      if (id.z == ids[k] && i + 2 < j) first[k] = i + 2;
-      if (id.y == ids[k] && i + 1 < j) first[k] = i + 1;
-      if (id.x == ids[k] && i < j) first[k] = i;
-    }
-  }
-  bool own[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    own[k] = ids[k] >= 0 && first[k] == lane + 64 * k;
-    if (!own[k]) val[k] = -INFINITY;
-  }
-  double em = wave_max64(l[0] > l[1] ? l[0] : l[1]);
-  if (em == -INFINITY) em = 0.;
-  const double vmax = a.tail ? 0. : wave_max64(val[0] > val[1] ? val[0] : val[1]);
-  const double vt = a.tail ? 1. : tau;
-  double e[2], p[2], lp[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    e[k] = ids[k] >= 0 ? exp((l[k] - em) / tau) : 0.;
-    lp[k] = own[k] ? (val[k] - vmax) / vt : -INFINITY;
-    p[k] = own[k] ? exp(lp[k]) : 0.;
-  }
-  const double se = wave_sum64((own[0] ? e[0] : 0.) + (own[1] ? e[1] : 0.));
-  const double sum = wave_sum64(p[0] + p[1]);
-  // A value that is a NaN or +infinity: no term of the row is a number.
-  const double bad = sum - sum, norm = a.tail ? 1. : sum, shift = a.tail ? 0. : log(sum);
-  double pl = 0.;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    p[k] = own[k] ? p[k] / norm + bad : 0.;
-    if (own[k] && !(p[k] == 0.)) pl += p[k] * (lp[k] - shift - (l[k] - em) / tau);
-    const int j = lane + 64 * k;
-    q.first[j] = first[k];
-    q.e[j] = e[k];
-    q.p[j] = p[k];
-  }
-  pl = wave_sum64(pl);
-  const bool none = __ballot(own[0] || own[1]) == 0;
-  if (lane == 0) {
-    q.em = em;
-    q.se = se;
-    q.sp = (a.tail ? sum : 1.) + bad;
-    q.pl = pl;
-    q.P = (a.tail && !(sum > 1.) ? 1. - sum : 0.) + bad;
-    q.none = none;
-  }
-  wave_sync();
 }
 
-// The same wave, with top and rest = sum exp((l - top) / tau) over the other logits: the loss,
-// the gradients' numbers and the state.
+// The entries' exponentials, by the first four of a block's waves (NTH threads): slot i's by
+// thread i, its value's by thread kTopMax + i.  Each wave finds the repeated ids and the two
+// maxima for itself, so that it waits for no other.
+template <int NTH>
+__device__ __forceinline__ void list_terms(const DistillArgs& a, List& q) {
+  if (threadIdx.x >= 2 * kTopMax) return;
+  const int lane = threadIdx.x & 63;
+  const int id0 = q.id[lane], id1 = q.id[lane + 64];
+  int f0 = lane, f1 = lane + 64;
+  for (int i = (a.m - 1) / 4 * 4; i >= 0; i -= 4) {
+    const int4 o = *reinterpret_cast<const int4*>(&q.id[i]);
+    f0 = o.w == id0 && i + 3 < f0 ? i + 3 : f0;
+    f0 = o.z == id0 && i + 2 < f0 ? i + 2 : f0;
+    f0 = o.y == id0 && i + 1 < f0 ? i + 1 : f0;
+    f0 = o.x == id0 && i < f0 ? i : f0;
+    f1 = o.w == id1 && i + 3 < f1 ? i + 3 : f1;
+    f1 = o.z == id1 && i + 2 < f1 ? i + 2 : f1;
+    f1 = o.y == id1 && i + 1 < f1 ? i + 1 : f1;
+    f1 = o.x == id1 && i < f1 ? i : f1;
+  }
+  const bool own0 = id0 >= 0 && f0 == lane, own1 = id1 >= 0 && f1 == lane + 64;
+  const float em = finite_top(wave_max(fmaxf(q.l[lane], q.l[lane + 64])));  // a NaN shows in its own term
+  const float vmax =
+      a.tail ? 0.f : wave_max(fmaxf(own0 ? q.val[lane] : -INFINITY, own1 ? q.val[lane + 64] : -INFINITY));
+  const double it = 1. / (double)a.x.tau;
+#pragma unroll 1
+  for (int t = threadIdx.x; t < 2 * kTopMax; t += NTH) {
+    const bool value = t >= kTopMax;
+    const int i = t & (kTopMax - 1);
+    const bool entry = value ? (i < 64 ? own0 : own1) : q.id[i] >= 0;
+    const double d = (value ? (double)q.val[i] - vmax : (double)q.l[i] - em) * (value && a.tail ? 1. : it);
+    (value ? q.p : q.e)[i] = entry ? exp(d) : 0.;
+    if (!value) q.first[i] = i < 64 ? f0 : f1;
+  }
+  if (threadIdx.x == 0) {
+    q.em = em;
+    q.vmax = vmax;
+  }
+}
+
+// One wave, once the terms are there, with top and rest = sum exp((l - top) / tau) over the other
+// logits: the loss, the gradients' numbers and the state.
 __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float top, double rest, int r) {
   const int lane = threadIdx.x & 63;
-  const double tau = a.x.tau;
-  // Sums relative to the larger maximum.
-  const bool over = rest != 0. && (q.se == 0. || top > q.em);
-  const double m = over ? (double)top : q.em;
-  const double fr = rest != 0. ? exp((top - m) / tau) : 0., fe = exp((q.em - m) / tau);
-  const double total = q.se * fe + rest * fr;
-  const double log_total = total > 0. ? log(total) : (double)nan_f();
-  const double scale = total > 0. ? fe / total : (double)nan_f();
-  if (lane == 0) {
-    double loss = q.pl + q.sp * (log_total + (m - q.em) / tau);
-    if (!(rest == 0.) && !(q.P == 0.)) loss += q.P * (log(q.P) - (log(rest) + (top - m) / tau - log_total));
-    a.loss[r] = q.none ? 0.f : (float)(tau * tau * loss);
-    q.k = rest == 0. ? (total > 0. ? 0.f : nan_f()) : (float)(tau * (fr / total - q.P / rest));
+  const double tau = a.x.tau, it = 1. / tau;
+  double se = 0., sum = 0.;
+  bool any = false;
+#pragma unroll 1
+  for (int j = lane; j < kTopMax; j += kWave) {
+    const bool own = q.id[j] >= 0 && q.first[j] == j;
+    any = any || own;
+    se += own ? q.e[j] : 0.;
+    sum += q.p[j];
   }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int j = lane + 64 * k;
-    if (q.id[j] >= 0) q.own[j] = (float)(tau * (q.e[j] * scale - q.p[j]));
+  se = wave_sum64(se);
+  sum = wave_sum64(sum);
+  const bool none = __ballot(any) == 0;
+  // A value that is a NaN or +infinity: no term of the row is a number.
+  const double bad = sum - sum, norm = a.tail ? 1. : 1. / sum;
+  const double P = (a.tail && !(sum > 1.) ? 1. - sum : 0.) + bad;
+  // The student's sums relative to the larger maximum; the first lane has the other logits'
+  // part, the second lane the entries'.
+  const bool over = rest != 0. && (se == 0. || top > q.em);
+  const double m = over ? (double)top : q.em, far = ((lane == 0 ? (double)top : q.em) - m) * it;
+  const double f = exp(far), fr = rest != 0. ? read_lane(f, 0) : 0., fe = read_lane(f, 1);
+  const double total = se * fe + rest * fr, odd = total > 0. && total < INFINITY ? 0. : (double)nan_f();
+  const double lg = log(lane == 0 ? rest : lane == 1 ? total : a.tail ? P : sum);
+  const double log_total = read_lane(lg, 1) + odd, log_mass = read_lane(lg, 2), part = 1. / total + odd;
+  const double shift = a.tail ? 0. : log_mass, vt = a.tail ? 1. : it;
+  double pl = 0.;
+#pragma unroll 1
+  for (int j = lane; j < kTopMax; j += kWave) {
+    if (q.id[j] < 0) continue;
+    const bool own = q.first[j] == j;
+    const double p = own ? q.p[j] * norm + bad : 0.;
+    q.own[j] = (float)(tau * (q.e[j] * fe * part - p));
+    if (own && !(p == 0.)) pl += p * (((double)q.val[j] - q.vmax) * vt - shift - ((double)q.l[j] - q.em) * it);
+  }
+  pl = wave_sum64(pl);
+  if (lane == 0) {
+    double loss = pl + ((a.tail ? sum : 1.) + bad) * (log_total + (m - q.em) * it);
+    if (!(rest == 0.) && !(P == 0.)) loss += P * (log_mass - (lg + far - log_total));
+    a.loss[r] = none ? 0.f : (float)(tau * tau * loss);
+    q.k = rest == 0. ? (float)odd : (float)(tau * (fr * part - P / rest));
+    q.none = none;
   }
   wave_sync();
   if (a.state == nullptr) return;
@@ -129,14 +131,11 @@ __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float to
   if (lane == 0) {
     st[0] = top;
     st[1] = q.k;
-    st[2] = q.none ? 1.f : 0.f;
+    st[2] = none ? 1.f : 0.f;
     st[3] = 0.f;
   }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int j = lane + 64 * k;
-    if (j < a.m) st[kState + j] = q.id[j] >= 0 ? q.own[q.first[j]] : 0.f;
-  }
+#pragma unroll 1
+  for (int j = lane; j < a.m; j += kWave) st[kState + j] = q.id[j] >= 0 ? q.own[q.first[j]] : 0.f;
 }
 
 template <typename T, int U>
@@ -163,7 +162,10 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a, Sp
   __shared__ List q;
   const int r = blockIdx.x;
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
-  take_list<T>(a, w, r, q);
+  fetch_list<T, kWave>(a, w, r, q);
+  wave_sync();
+  list_terms<kWave>(a, q);
+  wave_sync();
   const float4* parts = sp.parts + (int64_t)r * sp.chunks;
   float top = -INFINITY;
   for (int i = threadIdx.x; i < sp.chunks; i += kWave) top = fmaxf(top, parts[i].x);
@@ -204,8 +206,10 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(VocabRows x, int
     store1(const_cast<T*>(elem_at<T>(out, id)), own);
 }
 
-// Whole rows, one block each, and their gradient where one is asked for.  The first wave
-// takes the list (and the entries' logits, before any is overwritten) while the others load.
+// Whole rows, one block each, and their gradient where one is asked for.  The first waves
+// fetch the list before their logits (a load that comes behind those takes as long as all of
+// them: 12 of a row's 31 us at 2048 bf16 rows of 65537), and four of them take its
+// exponentials while the logits come.
 template <typename T, int NTH, int U>
 __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void distill_whole_kernel(DistillArgs a, RowGrad g) {
   __shared__ float red[3][NTH / 64];
@@ -213,13 +217,16 @@ __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void distill_whole_kernel
   __shared__ List q;
   const int r = blockIdx.x;
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
-  if (threadIdx.x < kWave) take_list<T>(a, w, r, q);
-  Tile<NTH, U> x;
-  load_tile<T>(x, w, 0);
   clear_marks(marks);
   __syncthreads();
-  if (threadIdx.x < kTopMax) set_mark(marks, w, 0, q.id[threadIdx.x]);
+  if (threadIdx.x < kTopMax) {
+    fetch_list<T, NTH>(a, w, r, q);
+    set_mark(marks, w, 0, q.id[threadIdx.x]);
+  }
+  Tile<NTH, U> x;
+  load_tile<T>(x, w, 0);
   __syncthreads();
+  list_terms<NTH>(a, q);
   const auto unlisted = [&](u32x4& s, int u) __attribute__((always_inline)) { drop_marked(s, u, marks); };
   const Part p = block_part<NTH>(a.x, tile_sums<T, true>(a.x, x, w, unlisted), red);
   const float top = finite_top(p.top);
@@ -258,7 +265,7 @@ template <typename T>
 hipError_t distill(const DistillArgs& a, const RowGrad& g, void* ws, hipStream_t s) {
   const int slots = slots_most<T>(a.x);
   if (slots <= kTileU * kThreads || (g.dlogits != nullptr && whole_row(a.x.rows, slots))) {
-    by_whole(slots, [&](auto k) {
+    by_whole<18>(slots, [&](auto k) {
       hipLaunchKernelGGL((distill_whole_kernel<T, k.kNth, k.kU>), dim3(a.x.rows), dim3(k.kNth), 0, s, a, g);
     });
     return note_hip(hipGetLastError());
