@@ -163,19 +163,37 @@ struct Tile {
   __device__ __forceinline__ int slot(int u) const { return slot0 + u * NTH + threadIdx.x; }
 };
 
-// Every thread loads U slots, without a branch, so that the wait for one does not wait for
-// those after it; a slot that is not a whole one of the row is read at the nearest that is
-// and replaced when it is taken (tile_sums) or not stored.
+// Slots are loaded and taken in batches of kRun, kAhead batches ahead of what is taken.  A wave issues
+// its instructions in order: with all of a long tile's loads before its first term, or many
+// batches ahead, the terms wait until the memory has room for those loads.  us, loss and
+// gradient of 1024 fp32 rows of 102400 (50 slots): all loads first 188; batches of four, 6
+// ahead 192, 2 ahead 182, 1 ahead 176; batches of eight, 1 ahead 176.
+constexpr int kRun = 8, kAhead = 1;
+
+// Batch b's loads.  Every thread loads every slot, without a branch, so that the wait for one
+// does not wait for those after it; a slot that is not a whole one of the row is read at
+// the nearest that is and replaced when it is taken (tile_sums) or not stored.
+template <int b, int NTH, int U>
+__device__ __forceinline__ void load_batch(Tile<NTH, U>& x, const Row& w) {
+  if (w.f0 < w.f1)
+    each<kRun>([&](auto i) __attribute__((always_inline)) {
+      constexpr int u = b * kRun + i;
+      if constexpr (u < U) x.x[u] = load_stream16(w.base + (uint32_t)min(max(x.slot(u), w.f0), w.f1 - 1) * 16u);
+    });
+}
+
+// The first kAhead batches; the others are loaded by tile_sums.
 template <typename T, int NTH, int U>
 __device__ __forceinline__ void load_tile(Tile<NTH, U>& x, const Row& w, int slot0) {
   x.slot0 = slot0;
   x.ragged = w.f1 < w.slots && w.slots > slot0;
   x.m = (w.slots - slot0 + NTH - 1) / NTH - x.ragged;
-  if (w.f0 < w.f1)
-    each<U>([&](auto u) __attribute__((always_inline)) {
-      x.x[u] = load_stream16(w.base + (uint32_t)min(max(x.slot(u), w.f0), w.f1 - 1) * 16u);
-    });
-  if (x.m > 0 && slot0 < w.f0) {
+  each<kAhead>([&](auto b) __attribute__((always_inline)) { load_batch<b>(x, w); });
+}
+// The row's first slot where the row starts inside it.
+template <typename T, int NTH, int U>
+__device__ __forceinline__ void load_first(Tile<NTH, U>& x, const Row& w) {
+  if (x.m > 0 && x.slot0 < w.f0) {
     x.x[0] = load_edge<T>(w, x.slot(0));
     // Waited for here: a load that only some rows have in flight would make all of them wait
     // for everything at their first slot.
@@ -333,12 +351,10 @@ __device__ __forceinline__ Part rebased(const VocabRows& x, const Part& p, float
   return Part{top, p.s * e, fmaf(p.s, d, p.w) * e};
 }
 
-// A thread's slots in batches of kRun, each as its loads arrive: waiting for all of them
-// and the row's maximum first left the memory idle while the terms were computed.  `fix`
-// may change a slot before it is taken.  With `nan` a NaN makes the sum one, else it
-// counts as -infinity.
-constexpr int kRun = 4;
-
+// A thread's slots in batches, each as its loads arrive: waiting for all of them and the
+// row's maximum first left the memory idle while the terms were computed.  `fix` may
+// change a slot before it is taken.  With `nan` a NaN makes the sum one, else it counts
+// as -infinity.
 template <typename T, bool nan, int NTH, int U, typename F>
 __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, const Row& w, const F& fix) {
   Part p{-INFINITY, 0.f, 0.f};
@@ -355,6 +371,8 @@ __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, c
   };
   each<(U + kRun - 1) / kRun>([&](auto b) __attribute__((always_inline)) {
     constexpr int u0 = b * kRun, k = U - u0 < kRun ? U - u0 : kRun;
+    load_batch<b + kAhead>(x, w);
+    if constexpr (u0 == 0) load_first<T>(x, w);
     if (u0 >= x.m) return;
     float top = p.top;
     each<k>([&](auto i) __attribute__((always_inline)) {

@@ -400,7 +400,9 @@ __global__ __launch_bounds__(kThreads) void scores_grad_kernel(VocabRows x, cons
   const ScoreGrad q = score_grad(x, tokens, g, r, st[0], st[1], st[2]);
   if (q.zero) return zero_tile<T, kThreads>(w, out, slot0);
   Tile<kThreads, U> l;
+  static_assert(U <= kAhead * kRun, "every slot is loaded at once");
   load_tile<T>(l, w, slot0);
+  load_first<T>(l, w);
   load_last<T>(l, w);
   if (q.ge == 0.f) scores_grad_tile<T, false>(x, q, l, w, out);
   else scores_grad_tile<T, true>(x, q, l, w, out);

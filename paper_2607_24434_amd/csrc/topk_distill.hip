@@ -187,7 +187,9 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(VocabRows x, int
   const float gr = g.g[r], top = st[0], k = st[1] * gr;
   if (gr == 0.f || st[2] != 0.f) return zero_tile<T, kThreads>(w, out, slot0);
   Tile<kThreads, U> l;
+  static_assert(U <= kAhead * kRun, "every slot is loaded at once");
   load_tile<T>(l, w, slot0);
+  load_first<T>(l, w);
   load_last<T>(l, w);
   const int j = threadIdx.x, id = j < m ? ids[(int64_t)r * m + j] : -1;
   const float own = j < m ? st[kState + j] * gr : 0.f;
@@ -219,13 +221,15 @@ __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void distill_whole_kernel
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);
   clear_marks(marks);
   __syncthreads();
+  Tile<NTH, U> x;
   if (threadIdx.x < kTopMax) {
     fetch_list<T, NTH>(a, w, r, q);
     set_mark(marks, w, 0, q.id[threadIdx.x]);
+  } else {
+    load_tile<T>(x, w, 0);
   }
-  Tile<NTH, U> x;
-  load_tile<T>(x, w, 0);
   __syncthreads();
+  if (threadIdx.x < kTopMax) load_tile<T>(x, w, 0);
   list_terms<NTH>(a, q);
   const auto unlisted = [&](u32x4& s, int u) __attribute__((always_inline)) { drop_marked(s, u, marks); };
   const Part p = block_part<NTH>(a.x, tile_sums<T, true>(a.x, x, w, unlisted), red);
