@@ -428,21 +428,22 @@ __device__ __forceinline__ void tile_groups(Tile<NTH, U>& x, const Row& w, int g
 // its slots that has one, so that the others cost a scalar test.
 template <typename T, int NTH, int U>
 struct Marks {
-  uint32_t bits[U * NTH * kE<T> / 32];
-  uint32_t slots[NTH / 64][(U + 31) / 32];
+  static constexpr int kWords = (U + 1) * NTH * kE<T> / 32, kFlags = (U + 32) / 32;  // with Tile::last
+  uint32_t bits[kWords];
+  uint32_t slots[NTH / 64][kFlags];
 };
 
 template <typename T, int NTH, int U>
 __device__ __forceinline__ void clear_marks(Marks<T, NTH, U>& k) {
-  for (int i = threadIdx.x; i < U * NTH * kE<T> / 32; i += NTH) k.bits[i] = 0;
+  for (int i = threadIdx.x; i < k.kWords; i += NTH) k.bits[i] = 0;
   if (threadIdx.x < NTH / 64)
-    for (int i = 0; i < (U + 31) / 32; ++i) k.slots[threadIdx.x][i] = 0;
+    for (int i = 0; i < k.kFlags; ++i) k.slots[threadIdx.x][i] = 0;
 }
 template <typename T, int NTH, int U>
 __device__ __forceinline__ void set_mark(Marks<T, NTH, U>& k, const Row& w, int slot0, int id) {
   if (id < 0 || id >= w.V) return;
   const int64_t e = (int64_t)id + w.o - (int64_t)slot0 * kE<T>;
-  if (e < 0 || e >= (int64_t)U * NTH * kE<T>) return;
+  if (e < 0 || e >= (int64_t)k.kWords * 32) return;
   const int i = (int)e, s = i / kE<T>, u = s / NTH, wave = s % NTH / 64;
   atomicOr(&k.bits[i >> 5], 1u << (i & 31));
   atomicOr(&k.slots[wave][u >> 5], 1u << (u & 31));
@@ -468,9 +469,12 @@ inline int slots_most(int V) {
   return (V + 2 * (kE<T> - 1)) / kE<T>;
 }
 template <typename T>
+inline bool at_slots(const VocabRows& x) {  // every row starts with a whole slot
+  return (reinterpret_cast<uintptr_t>(x.logits) & 15u) == 0 && x.ld % kE<T> == 0;
+}
+template <typename T>
 inline int slots_most(const VocabRows& x) {
-  const bool whole = (reinterpret_cast<uintptr_t>(x.logits) & 15u) == 0 && x.ld % kE<T> == 0;
-  return whole ? (x.V + kE<T> - 1) / kE<T> : slots_most<T>(x.V);
+  return at_slots<T>(x) ? (x.V + kE<T> - 1) / kE<T> : slots_most<T>(x.V);
 }
 
 // f with the smallest U that holds u slots a thread.
@@ -506,30 +510,42 @@ inline Split split_of(const VocabRows& x, int m, void* ws) {
 // Whole rows in one block's registers, which then write the gradient too: logits are read
 // once and gradients written once.  Threads and slots a thread; at most 512 threads of 256
 // registers, 50 slots of them the row's (102400 fp32 logits).
-constexpr int kWholeSlots = 512 * 50;
-
 template <int NTH, int U>
 struct Whole {
   static constexpr int kNth = NTH, kU = U;
 };
-// f with the smallest block that holds the slots.  Pair: the most slots a thread with which a
-// CU's registers hold two blocks, so that one computes while the other loads.
-template <int Pair, typename F>
-inline void by_whole(int slots, const F& f) {
-  if (slots <= 256) f(Whole<256, 1>{});
-  else if (slots <= 256 * 2) f(Whole<256, 2>{});
-  else if (slots <= 256 * 4) f(Whole<256, 4>{});
-  else if (slots <= 256 * 8) f(Whole<256, 8>{});
-  else if (slots <= 256 * 16) f(Whole<256, 16>{});
-  else if (slots <= 512 * 16) f(Whole<512, 16>{});
-  else if (slots <= 512 * Pair) f(Whole<512, Pair>{});
-  else f(Whole<512, 50>{});
+
+// Whether a tile of u slots a thread holds any of the rows: a row that ends inside a slot has
+// its last ones in Tile::last.
+template <typename T>
+inline bool holds(const VocabRows& x, int nth, int u) {
+  for (int o = 0; o < (at_slots<T>(x) ? 1 : kE<T>); ++o) {
+    const int64_t slots = ((int64_t)x.V + o + kE<T> - 1) / kE<T>, ragged = (x.V + o) % kE<T> != 0;
+    if (slots > (int64_t)nth * (u + ragged)) return false;
+  }
+  return true;
+}
+
+// f with the smallest block that holds the rows; false if none does.  Pair: the most slots a
+// thread with which a CU's registers hold two blocks, so that one computes while the other
+// loads.
+template <typename T, int Pair, typename F>
+inline bool by_whole(const VocabRows& x, const F& f) {
+  const auto take = [&](auto k) {
+    if (!holds<T>(x, k.kNth, k.kU)) return false;
+    f(k);
+    return true;
+  };
+  return take(Whole<256, 1>{}) || take(Whole<256, 2>{}) || take(Whole<256, 4>{}) || take(Whole<256, 8>{}) ||
+         take(Whole<256, 16>{}) || take(Whole<512, 16>{}) || take(Whole<512, Pair>{}) || take(Whole<512, 50>{});
 }
 // Waves of a SIMD that a block's registers leave room for.
 constexpr int whole_waves(int nth, int u) { return u < 50 ? 4 : nth / 256; }
 
-inline bool whole_row(int rows, int slots) {
-  return slots <= kWholeSlots && (slots <= kTileU * kThreads || rows >= 128);
+// Rows that a whole-row block serves better than parts: one tile's, or enough rows for the chip.
+template <typename T>
+inline bool whole_pays(const VocabRows& x, bool grad) {
+  return slots_most<T>(x) <= kTileU * kThreads || (grad && x.rows >= 128);
 }
 
 }  // namespace

@@ -450,12 +450,10 @@ hipError_t scores(const ScoresArgs& a, const RowGrad& g, void* ws, hipStream_t s
     });
     return note_hip(hipGetLastError());
   }
-  if (a.m == 0 && (slots <= kTileU * kThreads || (g.dlogits != nullptr && whole_row(a.x.rows, slots)))) {
-    by_whole<25>(slots, [&](auto k) {
-      hipLaunchKernelGGL((scores_whole_kernel<T, k.kNth, k.kU>), rows, dim3(k.kNth), 0, s, a, g);
-    });
+  if (a.m == 0 && whole_pays<T>(a.x, g.dlogits != nullptr) && by_whole<T, 25>(a.x, [&](auto k) {
+        hipLaunchKernelGGL((scores_whole_kernel<T, k.kNth, k.kU>), rows, dim3(k.kNth), 0, s, a, g);
+      }))
     return note_hip(hipGetLastError());
-  }
   const Split sp = split_of<T>(a.x, a.m, ws);
   by_u(sp.nu, [&](auto u) {
     hipLaunchKernelGGL((scores_part_kernel<T, u.value>), dim3((unsigned)a.x.rows * sp.chunks), dim3(kThreads), 0, s,

@@ -267,13 +267,10 @@ hipError_t distill_grad(const VocabRows& x, int m, const int32_t* ids, const flo
 
 template <typename T>
 hipError_t distill(const DistillArgs& a, const RowGrad& g, void* ws, hipStream_t s) {
-  const int slots = slots_most<T>(a.x);
-  if (slots <= kTileU * kThreads || (g.dlogits != nullptr && whole_row(a.x.rows, slots))) {
-    by_whole<18>(slots, [&](auto k) {
-      hipLaunchKernelGGL((distill_whole_kernel<T, k.kNth, k.kU>), dim3(a.x.rows), dim3(k.kNth), 0, s, a, g);
-    });
+  if (whole_pays<T>(a.x, g.dlogits != nullptr) && by_whole<T, 18>(a.x, [&](auto k) {
+        hipLaunchKernelGGL((distill_whole_kernel<T, k.kNth, k.kU>), dim3(a.x.rows), dim3(k.kNth), 0, s, a, g);
+      }))
     return note_hip(hipGetLastError());
-  }
   const Split sp = split_of<T>(a.x, 0, ws);
   by_u(sp.nu, [&](auto u) {
     hipLaunchKernelGGL((distill_part_kernel<T, u.value>), dim3((unsigned)a.x.rows * sp.chunks), dim3(kThreads), 0, s,

@@ -63,6 +63,11 @@ def near(got, want, tol):
     assert bad.size == 0, (bad[:5].tolist(), got[~same][:5], want[~same][:5], tol[~same][:5])
 
 
+def looked_at(rows):
+    """The rows that are compared: all of a few, else a dozen over them."""
+    return range(rows) if rows <= 16 else sorted({0, 1, rows // 2, rows - 2, rows - 1, *range(5, rows, rows // 7)})
+
+
 def logits(rng, rows, V):
     x = rng.normal(0, 2, (rows, V))
     for r in range(rows):
@@ -112,7 +117,7 @@ def run_scores(x, dtype, tau, tokens, m, pad=0, shift=0, g=None, ge=None, split=
 def check_scores(x, dtype, tau, tokens, m, g=None, ge=None, **kw):
     rows, V = x.shape
     held, logp, ent, idx, tlp, st, out = run_scores(x, dtype, tau, tokens, m, g=g, ge=ge, **kw)
-    for r in range(rows):
+    for r in looked_at(rows):
         gr, er = 0.0 if g is None else float(g[r]), 0.0 if ge is None else float(ge[r])
         lp, h, top, top_lp, grad = orc.scores(held[r], tau, int(tokens[r]), m, gr, er)
         near(logp[r:r + 1], [lp], [R(V) + 4 * U * abs(np.nan_to_num(lp, posinf=0, neginf=0))])
@@ -201,7 +206,8 @@ def test_rows_without_a_distribution(V, dtype):
 @pytest.mark.parametrize("split", [False, True])
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("rows,V", [(1, 1), (4, 1000), (3, 8200), (2, 50001), (300, 2049),
-                                    (260, 20011)])
+                                    (260, 20011), (130, 32769), (130, 65536), (129, 102397),
+                                    (128, 102400)])
 def test_scores_gradient(rows, V, in_place, split, dtype):
     rng = np.random.default_rng(rows + V)
     tokens = rng.integers(-1, V, rows)
@@ -259,7 +265,7 @@ def check_distill(x, dtype, ids, val, tail, tau, g=None, **kw):
     rows, V = x.shape
     held, loss, out = run_distill(x, dtype, ids, val, tail, tau, g, **kw)
     val = np.asarray(val, np.float32).astype(np.float64)
-    for r in range(rows):
+    for r in looked_at(rows):
         gr = 1.0 if g is None else float(np.float32(g[r]))
         want, grad = orc.distill(held[r], list(ids[r]), list(val[r]), tail, tau, gr)
         # Two logarithms of sums, weighted by at most one each; the rest is in 64 bits.
@@ -298,7 +304,8 @@ def test_distill(V, tail, dtype):
 @pytest.mark.parametrize("split", [False, True])
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("rows,V,m", [(1, 1, 1), (5, 1000, 8), (3, 8200, 64), (2, 50001, 128),
-                                      (300, 2049, 5), (260, 20011, 33)])
+                                      (300, 2049, 5), (260, 20011, 33), (130, 32769, 128),
+                                      (130, 65536, 9), (129, 102397, 100), (128, 102400, 64)])
 def test_distill_gradient(rows, V, m, in_place, split, dtype):
     rng = np.random.default_rng(rows + V)
     t = logits(rng, rows, V)
