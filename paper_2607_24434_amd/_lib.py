@@ -8,7 +8,6 @@ import of this module fails.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -238,7 +237,8 @@ def _ptr(t):
 def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    return torch.cuda.current_stream().cuda_stream
+    # The handle alone: torch.cuda.current_stream() makes an object of it in 2.7 us.
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _check(fn: str, rc: int):
@@ -635,40 +635,38 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
-def _device_of(t):
-    """The tensor's device as the current one, for a launch on one of its streams."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-        return torch.cuda.device(t.device)
-    return contextlib.nullcontext()
+def _launch(name, t, stream, *args):
+    """Calls the entry point on the tensor's device, by default on its current stream."""
+    fn = getattr(LIB, name)
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev >= 0 and dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream(stream))
+    else:
+        rc = fn(*args, _stream(stream))
+    if rc != 0:
+        _check(name, rc)
 
 
 def de_token_scores(rows, V, dtype, logits, ld, tau, tokens=None, logp=None, entropy=None, m=0,
                     top_idx=None, top_logp=None, stats=None, grad=None, ws=None, stream=None):
-    with _device_of(logits):
-        _check("de_token_scores", LIB.de_token_scores(
-            int(rows), int(V), int(dtype), _ptr(logits), int(ld), float(tau), _ptr(tokens), _ptr(logp),
-            _ptr(entropy), int(m), _ptr(top_idx), _ptr(top_logp), _ptr(stats), _ref(grad), _ptr(ws),
-            ws.numel() if ws is not None else 0, _stream(stream)))
+    _launch("de_token_scores", logits, stream, int(rows), int(V), int(dtype), _ptr(logits), int(ld),
+            float(tau), _ptr(tokens), _ptr(logp), _ptr(entropy), int(m), _ptr(top_idx),
+            _ptr(top_logp), _ptr(stats), _ref(grad), _ptr(ws), ws.numel() if ws is not None else 0)
 
 
 def de_token_scores_grad(rows, V, dtype, logits, ld, tau, tokens, stats, grad, stream=None):
-    with _device_of(logits):
-        _check("de_token_scores_grad", LIB.de_token_scores_grad(
-            int(rows), int(V), int(dtype), _ptr(logits), int(ld), float(tau), _ptr(tokens),
-            _ptr(stats), _ref(grad), _stream(stream)))
+    _launch("de_token_scores_grad", logits, stream, int(rows), int(V), int(dtype), _ptr(logits),
+            int(ld), float(tau), _ptr(tokens), _ptr(stats), _ref(grad))
 
 
 def de_topk_distill(rows, V, dtype, logits, ld, m, ids, values, tail, tau, loss, state=None,
                     grad=None, ws=None, stream=None):
-    with _device_of(logits):
-        _check("de_topk_distill", LIB.de_topk_distill(
-            int(rows), int(V), int(dtype), _ptr(logits), int(ld), int(m), _ptr(ids), _ptr(values),
-            int(tail), float(tau), _ptr(loss), _ptr(state), _ref(grad), _ptr(ws),
-            ws.numel() if ws is not None else 0, _stream(stream)))
+    _launch("de_topk_distill", logits, stream, int(rows), int(V), int(dtype), _ptr(logits), int(ld),
+            int(m), _ptr(ids), _ptr(values), int(tail), float(tau), _ptr(loss), _ptr(state),
+            _ref(grad), _ptr(ws), ws.numel() if ws is not None else 0)
 
 
 def de_topk_distill_grad(rows, V, dtype, logits, ld, m, ids, tau, state, grad, stream=None):
-    with _device_of(logits):
-        _check("de_topk_distill_grad", LIB.de_topk_distill_grad(
-            int(rows), int(V), int(dtype), _ptr(logits), int(ld), int(m), _ptr(ids), float(tau),
-            _ptr(state), _ref(grad), _stream(stream)))
+    _launch("de_topk_distill_grad", logits, stream, int(rows), int(V), int(dtype), _ptr(logits),
+            int(ld), int(m), _ptr(ids), float(tau), _ptr(state), _ref(grad))

@@ -544,12 +544,17 @@ constexpr int whole_waves(int nth, int u) { return u < 50 ? 4 : nth / 256; }
 
 // Rows that a whole-row block serves better than parts (which read a gradient's logits twice, but
 // put every CU on few long rows): a single tile's; with a gradient, rows short enough for one CU,
-// or enough of them for all.  us, loss and gradient, whole and parts: 1 row of 50000 fp32 16
+// or enough of them for all; without, where one launch saves more than the parts' finer
+// grain does.  us, loss and gradient, whole and parts: 1 row of 50000 fp32 16
 // and 17, 64 rows of 60000 bf16 17 and 17, of 102400 fp32 27 and 25, bf16 26 and 21, 128
 // rows 28 and 37, 27 and 28, 256 rows 40 and 65, 30 and 39.
+// Without a gradient, 64 rows of 50000 fp32 9.4 and 12, 256 12 and 12, 333 17 and 15.
 template <typename T>
 inline bool whole_pays(const VocabRows& x, bool grad) {
-  return slots_most<T>(x) <= kTileU * kThreads || (grad && (x.V <= 65536 || x.rows >= 100));
+  const int slots = slots_most<T>(x);
+  if (slots <= kTileU * kThreads) return true;
+  if (grad) return x.V <= 65536 || x.rows >= 100;
+  return x.V <= 65536 && x.rows <= 256;
 }
 
 }  // namespace
