@@ -220,7 +220,9 @@ __device__ __forceinline__ void each_slot(Tile<NTH, U>& x, const F& f) {
 template <typename T>
 __device__ __forceinline__ void store_slot(const Row& w, const Row& out, int s, const float (&v)[kE<T>]) {
   if (out.o == w.o && s >= w.f0 && s < w.f1) {
-    *(DE_GLOBAL u32x4*)(out.base + (int64_t)s * 16) = packed<T>(v);
+    // Past the caches: kept there, a large gradient pushes out the logits still to be read (us,
+    // gradients of 1024 fp32 rows of 102400 175 and 166, of 2048 bf16 rows 173 and 167).
+    __builtin_nontemporal_store(packed<T>(v), (DE_GLOBAL u32x4*)(out.base + (int64_t)s * 16));
     return;
   }
   each<kE<T>>([&](auto c) __attribute__((always_inline)) {
@@ -355,11 +357,14 @@ __device__ __forceinline__ Part rebased(const VocabRows& x, const Part& p, float
 // row's maximum first left the memory idle while the terms were computed.  `fix` may
 // change a slot before it is taken.  With `nan` a NaN makes the sum one, else it counts
 // as -infinity.
-template <typename T, bool nan, int NTH, int U, typename F>
-__device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, const Row& w, const F& fix) {
+template <typename T, bool nan, int NTH, int U, typename F, typename P>
+__device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, const Row& w, const F& fix, const P& peak) {
   Part p{-INFINITY, 0.f, 0.f};
-  const auto rise = [&](float& top, const u32x4& s) __attribute__((always_inline)) {
-    each<kE<T>>([&](auto c) __attribute__((always_inline)) { top = fmaxf(top, get<T>(s, c)); });
+  const auto rise = [&](float& top, const u32x4& s, int u) __attribute__((always_inline)) {
+    float v = -INFINITY;
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) { v = fmaxf(v, get<T>(s, c)); });
+    top = fmaxf(top, v);
+    peak(v, u);
   };
   const auto add = [&](const u32x4& s) __attribute__((always_inline)) {
     const float t = finite_top(p.top);
@@ -379,7 +384,7 @@ __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, c
       if (u0 + i >= x.m) return;
       if (x.slot0 + (u0 + i + 1) * NTH > w.f1 && x.slot(u0 + i) >= w.slots) x.x[u0 + i] = all_dropped<T>();
       fix(x.x[u0 + i], u0 + i);
-      rise(top, x.x[u0 + i]);
+      rise(top, x.x[u0 + i], u0 + i);
     });
     p = rebased(a, p, top);
     each<k>([&](auto i) __attribute__((always_inline)) {
@@ -390,7 +395,7 @@ __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, c
     load_last<T>(x, w);
     fix(x.last, x.m);
     float top = p.top;
-    rise(top, x.last);
+    rise(top, x.last, x.m);
     p = rebased(a, p, top);
     add(x.last);
   }
@@ -398,6 +403,9 @@ __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, c
 }
 struct NoFix {
   __device__ __forceinline__ void operator()(u32x4&, int) const {}
+};
+struct NoPeak {
+  __device__ __forceinline__ void operator()(float, int) const {}
 };
 
 // The parts of a block's threads as one.
@@ -410,18 +418,13 @@ __device__ __forceinline__ Part block_part(const VocabRows& a, Part p, float (*r
   return p;
 }
 
-// The maxima of groups of 2^glog slots (0, 2 or 4) of a tile: the best m logits lie in the m
-// groups whose (maximum, lower index) are best, so that only those are looked at again.
-template <typename T, int NTH, int U>
-__device__ __forceinline__ void tile_groups(Tile<NTH, U>& x, const Row& w, int glog, float* gm) {
-  const bool first = (threadIdx.x & ((1 << glog) - 1)) == 0;
-  each_slot(x, [&](const u32x4& s, int u) __attribute__((always_inline)) {
-    float v = -INFINITY;
-    each<kE<T>>([&](auto c) __attribute__((always_inline)) { v = fmaxf(v, get<T>(s, c)); });
-    if (glog == 4) v = row16_max(v);
-    else if (glog == 2) v = quad_max(v);
-    if (first && x.slot(u) < w.slots) gm[x.slot(u) >> glog] = v;
-  });
+// The maxima of groups of 2^glog slots (0, 2 or 4), from a slot's v: the best m logits lie in
+// the m groups whose (maximum, lower index) are best, so that only those are looked at
+// again.  All lanes of a wave.
+__device__ __forceinline__ void group_max(float v, int s, const Row& w, int glog, float* gm) {
+  if (glog == 4) v = row16_max(v);
+  else if (glog == 2) v = quad_max(v);
+  if ((threadIdx.x & ((1 << glog) - 1)) == 0 && s < w.slots) gm[s >> glog] = v;
 }
 
 // Marks of a tile's list entries: a bit for each logit, and for each wave a bit for each of

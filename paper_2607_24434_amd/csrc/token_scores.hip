@@ -12,7 +12,7 @@ namespace {
 // ---------------------------------------------------------------- the best m
 
 constexpr int kGroupCap = 1024;         // groups looked at again
-constexpr int kListCap = 9 * kThreads;  // logits: at least m + one round's of a block
+constexpr int kListCap = 4 * kThreads;  // logits: at least m and one of each thread (16 KB of both: 8 blocks a CU)
 constexpr int kSlack = 16;              // how many more than m a threshold may let through
 constexpr int kBatch = 8;               // slots a thread loads at once
 
@@ -288,8 +288,10 @@ __global__ __launch_bounds__(kThreads, 6) void scores_part_kernel(ScoresArgs a, 
   const Row w = until(row_at<T>(a.x.logits, a.x.ld, r, a.x.V), slot0 + sp.nu * kThreads);
   Tile<kThreads, U> x;
   load_tile<T>(x, w, slot0);
-  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{});
-  if (a.m > 0) tile_groups<T>(x, w, sp.glog, sp.gm + (int64_t)r * sp.gstride);
+  float* gm = sp.gm + (int64_t)r * sp.gstride;
+  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{}, [&](float v, int u) __attribute__((always_inline)) {
+    if (a.m > 0) group_max(v, x.slot(u), w, sp.glog, gm);
+  });
   const Part p = block_part<kThreads>(a.x, mine, red);
   if (threadIdx.x == 0) sp.parts[blockIdx.x] = make_float4(p.top, p.s, p.w, 0.f);
 }
@@ -336,8 +338,9 @@ __global__ __launch_bounds__(kThreads, 4) void scores_row_kernel(ScoresArgs a, i
   Tile<kThreads, U> x;
   load_tile<T>(x, w, 0);
   const float token = threadIdx.x == kWave ? token_logit<T>(a, w, r) : 0.f;
-  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{});
-  tile_groups<T>(x, w, glog, gm);
+  const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{}, [&](float v, int u) __attribute__((always_inline)) {
+    group_max(v, x.slot(u), w, glog, gm);
+  });
   const Part p = block_part<kThreads>(a.x, mine, red);
   const RowScore q = row_score(a.x, p);
   top_select<T>(w, gm, (w.slots + (1 << glog) - 1) >> glog, glog, a.m, a.x.tau, q.top, q.log_s,
@@ -418,7 +421,7 @@ __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void scores_whole_kernel(
   Tile<NTH, U> x;
   load_tile<T>(x, w, 0);
   if (threadIdx.x == 0) token = token_logit<T>(a, w, r);
-  const Part p = block_part<NTH>(a.x, tile_sums<T, false>(a.x, x, w, NoFix{}), red);
+  const Part p = block_part<NTH>(a.x, tile_sums<T, false>(a.x, x, w, NoFix{}, NoPeak{}), red);
   const RowScore q = row_score(a.x, p);
   if (threadIdx.x == 0) write_scores(a, r, q, token);
   if (g.dlogits == nullptr) return;

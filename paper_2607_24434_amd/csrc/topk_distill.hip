@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kThreads, 6) void distill_part_kernel(DistillArgs a
   set_mark(marks, w, slot0, id);
   __syncthreads();
   const auto unlisted = [&](u32x4& s, int u) __attribute__((always_inline)) { drop_marked(s, u, marks); };
-  const Part p = block_part<kThreads>(a.x, tile_sums<T, true>(a.x, x, w, unlisted), red);
+  const Part p = block_part<kThreads>(a.x, tile_sums<T, true>(a.x, x, w, unlisted, NoPeak{}), red);
   if (threadIdx.x == 0) sp.parts[blockIdx.x] = make_float4(p.top, p.s, p.w, 0.f);
 }
 
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(NTH, whole_waves(NTH, U)) void distill_whole_kernel
   if (threadIdx.x < kTopMax) load_tile<T>(x, w, 0);
   list_terms<NTH>(a, q);
   const auto unlisted = [&](u32x4& s, int u) __attribute__((always_inline)) { drop_marked(s, u, marks); };
-  const Part p = block_part<NTH>(a.x, tile_sums<T, true>(a.x, x, w, unlisted), red);
+  const Part p = block_part<NTH>(a.x, tile_sums<T, true>(a.x, x, w, unlisted, NoPeak{}), red);
   const float top = finite_top(p.top);
   if (threadIdx.x < kWave) end_list(a, q, top, (double)p.s + (double)a.x.corr * p.w, r);
   if (g.dlogits == nullptr) return;
