@@ -27,7 +27,7 @@ struct Split {
   int chunks;      // parts of a row
   int nu;          // slots a thread of a part, at most the kernel's U
   float4* parts;   // [rows, chunks]: maximum, sum e, sum e d
-  float* gm;       // [rows, gstride]: groups' maxima
+  uint32_t* gm;    // [rows, gstride]: groups' maxima
   int gstride, glog;
 };
 
@@ -361,8 +361,12 @@ template <typename T, bool nan, int NTH, int U, typename F, typename P>
 __device__ __forceinline__ Part tile_sums(const VocabRows& a, Tile<NTH, U>& x, const Row& w, const F& fix, const P& peak) {
   Part p{-INFINITY, 0.f, 0.f};
   const auto rise = [&](float& top, const u32x4& s, int u) __attribute__((always_inline)) {
+    // A signalling NaN is quieted first: a maximum with one is a NaN, and the logits before it
+    // are lost.  Where a NaN's sum shows it, that does not matter.
     float v = -INFINITY;
-    each<kE<T>>([&](auto c) __attribute__((always_inline)) { v = fmaxf(v, get<T>(s, c)); });
+    each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+      v = fmaxf(v, nan ? get<T>(s, c) : __builtin_canonicalizef(get<T>(s, c)));
+    });
     top = fmaxf(top, v);
     peak(v, u);
   };
@@ -418,13 +422,25 @@ __device__ __forceinline__ Part block_part(const VocabRows& a, Part p, float (*r
   return p;
 }
 
-// The maxima of groups of 2^glog slots (0, 2 or 4), from a slot's v: the best m logits lie in
-// the m groups whose (maximum, lower index) are best, so that only those are looked at
-// again.  All lanes of a wave.
-__device__ __forceinline__ void group_max(float v, int s, const Row& w, int glog, float* gm) {
-  if (glog == 4) v = row16_max(v);
-  else if (glog == 2) v = quad_max(v);
-  if ((threadIdx.x & ((1 << glog) - 1)) == 0 && s < w.slots) gm[s >> glog] = v;
+// The maxima of groups of 2^glog slots (0, 2 or 4) as whole numbers in their order, from a
+// slot's v (no NaN): the best m logits lie in the m groups whose (maximum, lower index) are
+// best, so that only those are looked at again.  All lanes of a wave.
+template <int ctrl>
+__device__ __forceinline__ uint32_t dpp_umax(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xF, 0xF, false));
+}
+__device__ __forceinline__ void group_max(float v, int s, const Row& w, int glog, uint32_t* gm) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  uint32_t k = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  if (glog > 0) {
+    k = dpp_umax<0xB1>(k);
+    k = dpp_umax<0x4E>(k);
+  }
+  if (glog == 4) {
+    k = dpp_umax<0x141>(k);
+    k = dpp_umax<0x140>(k);
+  }
+  if ((threadIdx.x & ((1 << glog) - 1)) == 0 && s < w.slots) gm[s >> glog] = k;
 }
 
 // Marks of a tile's list entries: a bit for each logit, and for each wave a bit for each of
@@ -506,7 +522,7 @@ inline Split split_of(const VocabRows& x, int m, void* ws) {
   sp.glog = group_log(slots);
   sp.gstride = m > 0 ? (slots >> sp.glog) + 1 : 0;
   sp.parts = static_cast<float4*>(ws);
-  sp.gm = reinterpret_cast<float*>(sp.parts + (int64_t)rows * sp.chunks);
+  sp.gm = reinterpret_cast<uint32_t*>(sp.parts + (int64_t)rows * sp.chunks);
   return sp;
 }
 

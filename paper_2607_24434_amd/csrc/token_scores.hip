@@ -74,23 +74,23 @@ __device__ __attribute__((noinline)) uint64_t prune(uint64_t* list, int& n_share
 //      logits).
 //   3. Each logit's rank in the list is its place.
 template <typename T, typename F>
-__device__ void top_select(const Row& w, const float* gm, int G, int glog, int m, float tau, float top,
+__device__ void top_select(const Row& w, const uint32_t* gm, int G, int glog, int m, float tau, float top,
                            float log_s, int32_t* idx, float* logp, TopShared& sh, const F& side) {
   const int tid = threadIdx.x;
   // The first kBatch groups of a thread stay in registers.
-  float v0[kBatch];
+  uint32_t v0[kBatch];
   each<kBatch>([&](auto i) __attribute__((always_inline)) {
     const int g = i * kThreads + tid;
-    v0[i] = g < G ? gm[g] : 0.f;
+    v0[i] = g < G ? gm[g] : 0;
   });
-  const auto group_key = [&](float v, int g) { return g < G ? order_key(v, g) : 0; };
+  const auto group_key = [&](uint32_t v, int g) { return g < G ? (uint64_t)v << 32 | (0xffffffffu - (uint32_t)g) : 0; };
   uint64_t best = 0;
   each<kBatch>([&](auto i) __attribute__((always_inline)) {
     const uint64_t k = group_key(v0[i], i * kThreads + tid);
     best = k > best ? k : best;
   });
   for (int g = kBatch * kThreads + tid; g < G; g += kThreads) {
-    const uint64_t k = order_key(gm[g], g);
+    const uint64_t k = group_key(gm[g], g);
     best = k > best ? k : best;
   }
   sh.list[tid] = best;
@@ -164,7 +164,7 @@ __device__ void top_select(const Row& w, const float* gm, int G, int glog, int m
       __syncthreads();  // every thread has read it before one appends
       if (full) bound = prune<kGroupCap>(sh.groups, sh.ngroups, m, sh);
       const int g = i * kThreads + tid;
-      const uint64_t k = g < G ? order_key(gm[g], g) : 0;
+      const uint64_t k = g < G ? group_key(gm[g], g) : 0;
       if (k >= bound) sh.groups[atomicAdd(&sh.ngroups, 1)] = k;
     }
   }
@@ -192,7 +192,9 @@ __device__ void top_select(const Row& w, const float* gm, int G, int glog, int m
     each<kBatch>([&](auto b) __attribute__((always_inline)) {
       if (j0 + b * kThreads >= work) return;
       float most = -INFINITY;
-      each<kE<T>>([&](auto c) __attribute__((always_inline)) { most = fmaxf(most, get<T>(x[b], c)); });
+      each<kE<T>>([&](auto c) __attribute__((always_inline)) {
+        most = fmaxf(most, __builtin_canonicalizef(get<T>(x[b], c)));
+      });
       if ((uint64_t)order_key(most) << 32 < (bound >> 32 << 32)) return;
 #pragma unroll 1
       for (int c = 0; c < kE<T>; ++c) {
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(kThreads, 6) void scores_part_kernel(ScoresArgs a, 
   const Row w = until(row_at<T>(a.x.logits, a.x.ld, r, a.x.V), slot0 + sp.nu * kThreads);
   Tile<kThreads, U> x;
   load_tile<T>(x, w, slot0);
-  float* gm = sp.gm + (int64_t)r * sp.gstride;
+  uint32_t* gm = sp.gm + (int64_t)r * sp.gstride;
   const Part mine = tile_sums<T, false>(a.x, x, w, NoFix{}, [&](float v, int u) __attribute__((always_inline)) {
     if (a.m > 0) group_max(v, x.slot(u), w, sp.glog, gm);
   });
@@ -331,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void scores_finish_kernel(ScoresArgs a, S
 template <typename T, int U>
 __global__ __launch_bounds__(kThreads, 4) void scores_row_kernel(ScoresArgs a, int glog) {
   __shared__ float red[3][kThreads / 64];
-  __shared__ float gm[U * kThreads];
+  __shared__ uint32_t gm[U * kThreads];
   __shared__ TopShared sh;
   const int r = blockIdx.x;
   const Row w = row_at<T>(a.x.logits, a.x.ld, r, a.x.V);

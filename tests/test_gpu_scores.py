@@ -185,6 +185,37 @@ def test_orders_ties_and_masked_logits(V, m, dtype):
     check_scores(x, dtype, 1.0, tokens, 0, g=np.linspace(-1, 1, n), ge=np.linspace(0.5, 1, n))
 
 
+@pytest.mark.parametrize("bits,dtype", [(0x7F800001, torch.float32), (-0x7EDCBB, torch.float32),
+                                        (0x7F81, torch.bfloat16), (-0x7E, torch.bfloat16)])
+@pytest.mark.parametrize("V", [900, 30000])
+def test_a_nan_of_any_bits_counts_as_minus_infinity(V, bits, dtype):
+    """Signalling NaNs too, which memory that nothing wrote may hold; a loss shows them."""
+    rng = np.random.default_rng(V)
+    rows, m = 3, 40
+    x = torch.from_numpy(logits(rng, rows, V)).to("cuda").to(dtype)
+    plain = x.clone()
+    at = torch.from_numpy(rng.permutation(V)[:V // 3]).to("cuda")
+    x.view(torch.int32 if dtype == torch.float32 else torch.int16)[:, at] = bits
+    assert bool(torch.isnan(x[:, at]).all())
+    plain[:, at] = float("-inf")
+    got = []
+    for t in (x, plain):
+        idx, tlp, logp, ent = full(rows, m, value=-7, dtype=torch.int32), full(rows, m), full(rows), full(rows)
+        d = full(rows, V, dtype=dtype)
+        ws = de.scores_workspace(rows, V, m)
+        tok = i32([0, 1, 2])
+        de.de_token_scores(rows, V, CODE[dtype], t, V, 1.0, tok, logp, ent, m, idx, tlp, ws=ws)
+        de.de_token_scores(rows, V, CODE[dtype], t, V, 1.0, tok, logp,
+                           grad=de.make_row_grad(f32(np.ones(rows)), d, V), ws=ws)
+        got.append((idx, tlp, logp, ent, d))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    loss, d = full(rows, value=0.0), full(rows, V, value=0.0, dtype=dtype)
+    de.de_topk_distill(rows, V, CODE[dtype], x, V, m, idx, tlp, 1, 1.0, loss,
+                       grad=de.make_row_grad(f32(np.ones(rows)), d, V), ws=ws)
+    assert bool(torch.isnan(loss).all()) and bool(torch.isnan(d).all())
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("V", [5, 3000, 50000])
 def test_rows_without_a_distribution(V, dtype):
