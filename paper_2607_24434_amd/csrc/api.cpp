@@ -1394,6 +1394,9 @@ int de_row_kl(int rows, int n, const float* a, int lda, const float* b, int ldb,
 
 namespace {
 
+static_assert(DE_TOP_MAX == de::kTopMax && DE_SCORE_STATS == de::kStats && DE_DISTILL_STATE == de::kState,
+              "the header's sizes are the kernels'");
+
 // The scratch of a vocabulary call: what its launches exchange, then the rows' statistics
 // or state where the caller keeps none.
 size_t scores_state_at(int rows, int V, int m) { return up256(de::scores_bytes(rows, V, m)); }

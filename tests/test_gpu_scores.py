@@ -69,7 +69,8 @@ def looked_at(rows):
 
 
 def logits(rng, rows, V):
-    x = rng.normal(0, 2, (rows, V))
+    # Many rows share 17 rows' noise and differ in their likely tokens.
+    x = rng.normal(0, 2, (min(rows, 17), V))[np.arange(rows) % 17]
     for r in range(rows):
         at = rng.integers(0, V, 5)
         x[r, at] = rng.uniform(3, 12, 5)
@@ -238,7 +239,7 @@ def test_rows_without_a_distribution(V, dtype):
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("rows,V", [(1, 1), (4, 1000), (3, 8200), (2, 50001), (300, 2049),
                                     (260, 20011), (130, 32769), (130, 65536), (129, 102397),
-                                    (128, 102400)])
+                                    (128, 102400), (3, 70001), (100, 102409)])
 def test_scores_gradient(rows, V, in_place, split, dtype):
     rng = np.random.default_rng(rows + V)
     tokens = rng.integers(-1, V, rows)
@@ -336,7 +337,8 @@ def test_distill(V, tail, dtype):
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("rows,V,m", [(1, 1, 1), (5, 1000, 8), (3, 8200, 64), (2, 50001, 128),
                                       (300, 2049, 5), (260, 20011, 33), (130, 32769, 128),
-                                      (130, 65536, 9), (129, 102397, 100), (128, 102400, 64)])
+                                      (130, 65536, 9), (129, 102397, 100), (128, 102400, 64),
+                                      (3, 70001, 128), (100, 102409, 20)])
 def test_distill_gradient(rows, V, m, in_place, split, dtype):
     rng = np.random.default_rng(rows + V)
     t = logits(rng, rows, V)
@@ -381,6 +383,57 @@ def test_a_list_of_the_whole_vocabulary_has_no_tail():
     t = logits(rng, 3, 100)
     ids, val = lists(rng, t, 128, True, 1.0, ragged=False)
     check_distill(t + rng.normal(0, 1, t.shape), torch.float32, ids, val, True, 1.0, g=np.ones(3))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(4, 1003), (3, 20000), (2, 80001)])
+def test_gradients_at_other_elements_than_the_logits(rows, V, dtype):
+    """dlogits with a row length and a start of its own: the same gradient to the bit."""
+    rng = np.random.default_rng(V)
+    t, ld, _ = placed(logits(rng, rows, V), dtype, 3, 1)
+    tok, g = i32(rng.integers(0, V, rows)), f32(rng.normal(0, 1, rows))
+    ids, val = lists(rng, t[:, :V].float().cpu().numpy(), 17, True, 1.0)
+    ws = de.scores_workspace(rows, V)
+    got = []
+    for pad, shift in ((3, 1), (6, 3), (0, 0)):
+        base = full(rows * (V + pad) + shift, value=3.0, dtype=dtype)
+        out = base[shift:].view(rows, V + pad)
+        grad = de.make_row_grad(g, out, V + pad)
+        de.de_token_scores(rows, V, CODE[dtype], t, ld, 1.0, tok, grad=grad, ws=ws)
+        a = out[:, :V].clone()
+        de.de_topk_distill(rows, V, CODE[dtype], t, ld, 17, i32(ids), f32(val), 1, 1.0, full(rows),
+                           grad=grad, ws=ws)
+        got.append((a, out[:, :V].clone()))
+        assert bool((out[:, V:] == 3.0).all()) and bool((base[:shift] == 3.0).all())
+    for a, b in got[1:]:
+        assert torch.equal(a, got[0][0]) and torch.equal(b, got[0][1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 7, 100, 600])
+@pytest.mark.parametrize("V", [1, 2047, 8190, 8192, 8194, 16384, 16390, 32766, 65537])
+def test_nothing_past_the_scratch(V, rows, dtype):
+    """The calls' scratch is all that they use of it, rows at whole slots and at any element."""
+    m, guard = min(V, 11), 4096
+    base = torch.randn(rows * (V + 1) + 8, device="cuda").to(dtype)
+    tok = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    g = torch.ones(rows, device="cuda")
+    d = full(rows, V, dtype=dtype)
+    for shift, ld in ((0, (V + 7) // 8 * 8 if rows * ((V + 7) // 8 * 8) <= base.numel() else V), (1, V + 1)):
+        t = base[shift:]
+        for k in (m, 0):
+            n = de.de_scores_workspace_bytes(rows, V, k)
+            ws = torch.full((n + guard,), 171, dtype=torch.uint8, device="cuda")
+            args = (rows, V, CODE[dtype], t, ld)
+            grad = de.make_row_grad(g, d, V)
+            idx, tlp = full(rows, m, value=-7, dtype=torch.int32), full(rows, m)
+            if k:
+                de.de_token_scores(*args, 1.0, tok, full(rows), m=k, top_idx=idx, top_logp=tlp, ws=ws[:n])
+                assert int(idx.min()) >= 0 and int(idx.max()) < V
+            else:
+                de.de_token_scores(*args, 1.0, tok, full(rows), grad=grad, ws=ws[:n])
+                de.de_topk_distill(*args, m, idx.clamp(min=0), tlp, 0, 1.0, full(rows), grad=grad, ws=ws[:n])
+            assert bool((ws[n:] == 171).all())
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
