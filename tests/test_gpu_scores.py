@@ -436,6 +436,46 @@ def test_nothing_past_the_scratch(V, rows, dtype):
             assert bool((ws[n:] == 171).all())
 
 
+@pytest.mark.parametrize("rows,V,m", [(200000, 7, 3), (1 << 20, 1, 1), (70001, 130, 20),
+                                      (2, 20000003, 128)])
+def test_many_rows_and_long_ones(rows, V, m):
+    """Against 64 bits on the GPU: more rows than a grid's other dimensions take, and a row of
+    twenty million."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.empty(rows, V, device="cuda").normal_(0, 3, generator=gen)
+    tok = torch.randint(V, (rows,), generator=gen, device="cuda").int()
+    g = torch.empty(rows, device="cuda").normal_(generator=gen)
+    idx, tlp, logp, ent = full(rows, m, value=-7, dtype=torch.int32), full(rows, m), full(rows), full(rows)
+    d, loss, dl = full(rows, V), full(rows), full(rows, V)
+    ws = de.scores_workspace(rows, V, m)
+    de.de_token_scores(rows, V, de.DE_F32, x, V, 1.0, tok, logp, ent, m, idx, tlp, ws=ws)
+    de.de_token_scores(rows, V, de.DE_F32, x, V, 1.0, tok, grad=de.make_row_grad(g, d, V), ws=ws)
+    lp = torch.log_softmax(x.double(), 1)
+    p = lp.exp()
+    want = lp.gather(1, tok.long()[:, None])[:, 0]
+    assert bool(((logp - want).abs() <= R(V) + 4 * U * want.abs()).all())
+    assert bool(((ent + (p * lp).sum(1)).abs() <= 2 * R(V) * (2 + math.log(V))).all())
+    best = lp.topk(m, 1)
+    assert bool(((tlp - best.values).abs() <= R(V) + 4 * U * best.values.abs()).all())
+    assert torch.equal(x.gather(1, idx.long()), x.gather(1, best.indices))
+    assert m == 1 or bool(((tlp[:, 1:] < tlp[:, :-1]) | (idx[:, 1:] != idx[:, :-1])).all())
+    want = -p * g[:, None].double()
+    want.scatter_add_(1, tok.long()[:, None], g.double()[:, None])
+    # p's error, with its argument's share, and the token's own rounding.
+    tol = p * g.abs()[:, None] * (2 * R(V) + 8 * U * (lp.abs() + math.log(V))) + 1e-37
+    tol.scatter_add_(1, tok.long()[:, None], 4 * U * g.abs().double()[:, None])
+    assert bool(((d - want).abs() <= tol).all())
+    # Distillation towards the row's own best entries: p = q / (1 - Q), loss -log(1 - Q).
+    de.de_topk_distill(rows, V, de.DE_F32, x, V, m, idx, x.gather(1, idx.long()), 0, 1.0, loss,
+                       grad=de.make_row_grad(g, dl, V), ws=ws)
+    mass = p.gather(1, idx.long()).sum(1, keepdim=True)
+    assert bool(((loss + mass[:, 0].log()).abs() <= 2 * R(V) + 2 * U * mass[:, 0].log().abs()).all())
+    dist = torch.zeros_like(p).scatter_(1, idx.long(), p.gather(1, idx.long()) / mass)
+    want = (p - dist) * g[:, None].double()
+    tol = (p + dist) * g.abs()[:, None] * (2 * R(V) + 8 * U * (lp.abs() + math.log(V))) + 1e-37
+    assert bool(((dl - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_offsets_beyond_32_bits(dtype):
     """Rows 2^30 + 8 elements apart: the last one starts past 2^31 elements."""
