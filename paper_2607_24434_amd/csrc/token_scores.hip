@@ -2,8 +2,13 @@
 //
 // With M = max l and S = sum_v exp((l_v - M) / tau):
 //   log p_v = (l_v - M) / tau - log S,     H = log S - (sum_v e_v d_v) / S
-// (e_v the summand, d_v = (l_v - M) / tau).  Differences to the maximum are taken before
-// they are scaled, so that logits far from zero lose nothing.
+// (e_v the summand, d_v = (l_v - M) / tau), and for the gradient
+//   d (g log p_t + h H) / d l_v = (g (1[v = t] - p_v) - h p_v (log p_v + H)) / tau.
+// Differences to the maximum are taken before they are scaled, so that logits far from zero
+// lose nothing.  Memory bounds the long rows (2048 fp32 rows of 102400: parts 136 us, 6.2 TB/s;
+// bf16 with the gradient from the same registers 159 us, 5.3 TB/s), the vector ALU bf16 parts (19
+// instruction slots a logit), a chain of dependent steps the alternatives (7 us a row, 22
+// for 2048).
 #include "scores_core.h"
 
 namespace de {
