@@ -676,8 +676,10 @@ int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld,
  * a logit of -infinity gives an infinite loss.
  *   state [rows, m + DE_DISTILL_STATE] (may be NULL): for de_topk_distill_grad;
  *   grad (may be NULL): the logits' gradient out of the same call,
- *     dlogits_v = g tau (q_v - p_v) for entries, g tau q_v (1 - P / Q) for the other
- *     tokens (P = 0 with tail = 0). */
+ *     dlogits_v = g tau (W q_v - p_v) for entries, g tau q_v (W - P / Q) for the other
+ *     tokens, W = sum_S p_j + P (1 and P = 0 with tail = 0).  W is 1 unless sum_S p_j is
+ *     more (log probabilities stored in few bits may sum to that), or the last term is
+ *     left out, and P with it (then sum_S p_j).  A row's gradient sums to zero. */
 int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int m,
                     const int32_t* ids, const float* values, int tail, float tau, float* loss,
                     float* state, const de_row_grad* grad, void* ws, size_t ws_bytes,

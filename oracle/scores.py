@@ -77,7 +77,7 @@ def distill(l, ids, values, tail, tau, g=1.0):
         loss = np.sum(p[on] * (lp[on] - lq[s][on]))
         rest = np.ones(V, bool)
         rest[s] = False
-        ratio = 0.0
+        ratio, weight = 0.0, np.sum(p) if tail else 1.0  # weight: of log sum exp(l / tau) in the loss
         if tail and np.any(l[rest] > -np.inf):
             big = max(0.0, 1.0 - np.sum(p))
             r = l[rest]
@@ -89,6 +89,7 @@ def distill(l, ids, values, tail, tau, g=1.0):
                 # q_v P / Q without Q's underflow
                 ratio = np.zeros(V)
                 ratio[rest] = big * np.exp(d) / np.sum(np.exp(d))
-    grad = q - ratio
-    grad[s] = q[s] - p
+                weight += big
+    grad = weight * q - ratio
+    grad[s] = weight * q[s] - p
     return tau * tau * loss, (g * tau * grad if g != 0 else np.zeros(V))

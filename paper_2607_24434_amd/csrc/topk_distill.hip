@@ -3,7 +3,9 @@
 // With q = softmax(l / tau), p the teacher's probabilities of the list's entries S, P its mass
 // outside them (0 unless asked for) and Q = sum_{v not in S} q_v:
 //   loss = tau^2 (sum_S p (log p - log q) + P (log P - log Q))
-//   d loss / d l_v = tau (q_v - p_v) in S, tau q_v (1 - P / Q) outside.
+//   d loss / d l_v = tau (W q_v - p_v) in S, tau q_v (W - P / Q) outside,
+// W = sum_S p + P the weight of log sum exp(l / tau).  W is one unless the list's own masses
+// are more than that (P = 0), or the student has no mass outside the list (P's term is left out).
 // The logits outside the list are summed directly: one minus the entries' mass would lose a
 // small Q.  Memory bounds it: a whole row is read once and its gradient written once from the
 // same registers (1024 fp32 rows of 102400 with lists of 64: 166 us, 5.1 TB/s where a copy
@@ -23,8 +25,8 @@ struct List {
   double p[kTopMax];       // exp(value - vmax), 0 but in first slots
   float em, vmax;          // the entries' largest logit; the largest value (0 with tail)
   // Once the sum over the other logits is known:
-  float own[kTopMax];      // an entry's gradient tau (q - p), in its first slot
-  float k;                 // tau (Q - P) / (sum outside): the others' is k exp((l - top) / tau)
+  float own[kTopMax];      // an entry's gradient tau (W q - p), in its first slot
+  float k;                 // tau (W Q - P) / (sum outside): the others' is k exp((l - top) / tau)
   int none;                // no entry at all
 };
 
@@ -115,13 +117,14 @@ __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float to
   const double lg = log(lane == 0 ? rest : lane == 1 ? total : a.tail ? P : sum);
   const double log_total = read_lane(lg, 1) + odd, log_mass = read_lane(lg, 2), part = 1. / total + odd;
   const double shift = a.tail ? 0. : log_mass, vt = a.tail ? 1. : it;
+  const double W = a.tail ? sum + (rest != 0. ? P : bad) : 1.;
   double pl = 0.;
 #pragma unroll 1
   for (int j = lane; j < kTopMax; j += kWave) {
     if (q.id[j] < 0) continue;
     const bool own = q.first[j] == j;
     const double p = own ? q.p[j] * norm + bad : 0.;
-    q.own[j] = (float)(tau * (q.e[j] * fe * part - p));
+    q.own[j] = (float)(tau * (W * (q.e[j] * fe * part) - p));
     if (own && !(p == 0.)) pl += p * (((double)q.val[j] - q.vmax) * vt - shift - ((double)q.l[j] - q.em) * it);
   }
   pl = wave_sum64(pl);
@@ -129,7 +132,7 @@ __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float to
     double loss = pl + ((a.tail ? sum : 1.) + bad) * (log_total + (m - q.em) * it);
     if (!(rest == 0.) && !(P == 0.)) loss += P * (log_mass - (lg + far - log_total));
     a.loss[r] = none ? 0.f : (float)(tau * tau * loss);
-    q.k = rest == 0. ? (float)odd : (float)(tau * (fr * part - P / rest));
+    q.k = rest == 0. ? (float)odd : (float)(tau * (W * fr * part - P / rest));
     q.none = none;
   }
   wave_sync();
