@@ -109,10 +109,10 @@ __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float to
   const double bad = sum - sum, norm = a.tail ? 1. : 1. / sum;
   const double P = (a.tail && !(sum > 1.) ? 1. - sum : 0.) + bad;
   // The student's sums relative to the larger maximum; the first lane has the other logits'
-  // part, the second lane the entries'.
+  // part, the second lane the entries'; a side without any mass has no maximum, and none is taken.
   const bool over = rest != 0. && (se == 0. || top > q.em);
   const double m = over ? (double)top : q.em, far = ((lane == 0 ? (double)top : q.em) - m) * it;
-  const double f = exp(far), fr = rest != 0. ? read_lane(f, 0) : 0., fe = read_lane(f, 1);
+  const double f = exp(far), fr = rest != 0. ? read_lane(f, 0) : 0., fe = se != 0. ? read_lane(f, 1) : 0.;
   const double total = se * fe + rest * fr, odd = total > 0. && total < INFINITY ? 0. : (double)nan_f();
   const double lg = log(lane == 0 ? rest : lane == 1 ? total : a.tail ? P : sum);
   const double log_total = read_lane(lg, 1) + odd, log_mass = read_lane(lg, 2), part = 1. / total + odd;

@@ -133,3 +133,21 @@ def test_a_list_of_the_vocabulary_of_any_mass(mass, split, dtype):
     x, ids, val = teacher(rng, 3, 100, 100, 1.0)
     val = np.stack([with_mass(v, mass) for v in val])
     check(x, dtype, ids, val, 1, 1.0, np.ones(3), split)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("at,tau", [(-1000.0, 1.0), (-30.0, 0.01), (1000.0, 1.0), (0.0, 1.0)])
+@pytest.mark.parametrize("V", SIZES)
+def test_a_student_that_gives_the_list_nothing(V, at, tau, split, dtype):
+    """An infinite loss, or a finite one where the teacher's mass is all outside the list, and
+    a finite gradient, wherever the other logits lie."""
+    rng = np.random.default_rng(V + 1)
+    x, ids, val = teacher(rng, 4, V, 24, 1.0)
+    np.put_along_axis(x, ids.astype(np.int64), -np.inf, 1)
+    x += at
+    ids[1, 3:] = -1
+    val[3] = -np.inf
+    g = np.linspace(0.5, 2.0, 4)
+    check(x, dtype, ids, val, 1, tau, g, split)
+    check(x[:3], dtype, ids[:3], val[:3], 0, tau, g[:3], split)
