@@ -671,8 +671,8 @@ int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld,
  * An id outside [0, V) (such as -1) and an id that an earlier slot of its row holds
  * are no entries: their values do not count.  A row without entries has loss 0 and a
  * zero gradient, whatever its logits hold.  A NaN or +infinity among a row's logits,
- * or in an entry's value, gives a NaN loss and gradient, and so does a list of
- * -infinities with tail = 0; an entry with p_j = 0 adds nothing, one with p_j > 0 and
+ * or in an entry's value, gives a NaN loss and gradient, and so do logits that are all
+ * -infinity, and a list of -infinities with tail = 0; an entry with p_j = 0 adds nothing, one with p_j > 0 and
  * a logit of -infinity gives an infinite loss.
  *   state [rows, m + DE_DISTILL_STATE] (may be NULL): for de_topk_distill_grad;
  *   grad (may be NULL): the logits' gradient out of the same call,

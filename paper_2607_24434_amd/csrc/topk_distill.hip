@@ -132,7 +132,7 @@ __device__ __forceinline__ void end_list(const DistillArgs& a, List& q, float to
     double loss = pl + ((a.tail ? sum : 1.) + bad) * (log_total + (m - q.em) * it);
     if (!(rest == 0.) && !(P == 0.)) loss += P * (log_mass - (lg + far - log_total));
     a.loss[r] = none ? 0.f : (float)(tau * tau * loss);
-    q.k = rest == 0. ? (float)odd : (float)(tau * (W * fr * part - P / rest));
+    q.k = rest == 0. ? (float)(odd + bad) : (float)(tau * (W * fr * part - P / rest));
     q.none = none;
   }
   wave_sync();

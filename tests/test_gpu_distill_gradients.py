@@ -151,3 +151,21 @@ def test_a_student_that_gives_the_list_nothing(V, at, tau, split, dtype):
     g = np.linspace(0.5, 2.0, 4)
     check(x, dtype, ids, val, 1, tau, g, split)
     check(x[:3], dtype, ids[:3], val[:3], 0, tau, g[:3], split)
+
+
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("V", [300, 9000, 70001])
+def test_values_that_are_no_numbers(V, tail, split):
+    """A NaN loss and gradient, the tokens that the student gives nothing among them."""
+    rng = np.random.default_rng(V + 2)
+    x, ids, val = teacher(rng, 6, V, 24, 1.0)
+    val[0, 3], val[1, 0], val[2, 5] = np.nan, np.inf, np.nan
+    for r in (0, 1, 3):  # nothing outside the list
+        keep = x[r, ids[r]].copy()
+        x[r] = -np.inf
+        x[r, ids[r]] = keep
+    val[3] = -np.inf  # no distribution with tail = 0, no entry's mass with tail = 1
+    x[4] = -np.inf
+    ids[5, 7], val[5, 7] = -1, np.nan  # not an entry
+    check(x, torch.float32, ids, val, tail, 1.0, np.linspace(0.5, 2.0, 6), split)
