@@ -47,6 +47,30 @@ def near(got, want, tol, what):
     assert bad.size == 0, (what, bad.tolist(), got[~ok][:5], want[~ok][:5], tol[~ok][:5])
 
 
+def tolerances(l, ids, val, tail, tau, g, want, wgrad, dtype):
+    """Of one row's loss and of its gradient."""
+    V = l.size
+    slots = orc.entries(list(ids), V)
+    at = [ids[j] for j in slots]
+    v = val[slots] if tail else orc.log_softmax(val[slots], tau)
+    mass = 1.0 if not tail or not np.isfinite(v).any() else float(np.sum(np.exp(v)))
+    total = mass + max(0.0, 1.0 - mass)
+    # The logarithms of the sums carry weights of mass and P at most, twice.
+    loss_tol = tau * tau * 2 * total * R(V) + 2 * U * abs(np.nan_to_num(want, posinf=0.0))
+    if not np.isfinite(wgrad).all():
+        return loss_tol, 0.0
+    lq = np.maximum(orc.log_softmax(l, tau), -1000.0)
+    q = np.exp(lq)
+    # q_v W and q_v P / Q each with R(V) and the argument's share; P / Q from the gradient
+    # itself.
+    both = tau * abs(g) * q * total + np.abs(tau * g * q * total - wgrad)
+    tol = both * (R(V) + U * (8 + 3 * np.abs(lq))) + 1e-37
+    tol[at] = tau * abs(g) * total * q[at] * R(V) + 4 * U * np.abs(wgrad[at]) + 1e-37
+    if dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (np.abs(wgrad) + tol)
+    return loss_tol, tol
+
+
 def check(x, dtype, ids, val, tail, tau, g, split):
     """Loss and gradient of every row against the oracle; a finite gradient sums to zero."""
     rows, V = x.shape
@@ -69,25 +93,9 @@ def check(x, dtype, ids, val, tail, tau, g, split):
     for r in range(rows):
         gr = float(np.float32(g[r]))
         want, wgrad = orc.distill(held[r], list(ids[r]), list(val[r]), tail, tau, gr)
-        slots = orc.entries(list(ids[r]), V)
-        at = [ids[r][j] for j in slots]
-        v = val[r][slots] if tail else orc.log_softmax(val[r][slots], tau)
-        mass = 1.0 if not tail or not np.isfinite(v).any() else float(np.sum(np.exp(v)))
-        total = mass + max(0.0, 1.0 - mass)
-        # The logarithms of the sums carry weights of mass and P at most, twice.
-        near(loss[r:r + 1], np.asarray([want]),
-             tau * tau * 2 * total * R(V) + 2 * U * abs(np.nan_to_num(want, posinf=0.0)), (r, "loss"))
-        tol = 0.0
+        loss_tol, tol = tolerances(held[r], ids[r], val[r], tail, tau, gr, want, wgrad, dtype)
+        near(loss[r:r + 1], np.asarray([want]), loss_tol, (r, "loss"))
         if np.isfinite(wgrad).all():
-            lq = np.maximum(orc.log_softmax(held[r], tau), -1000.0)
-            q = np.exp(lq)
-            # q_v W and q_v P / Q each with R(V) and the argument's share; P / Q from the
-            # gradient itself.
-            both = tau * abs(gr) * q * total + np.abs(tau * gr * q * total - wgrad)
-            tol = both * (R(V) + U * (8 + 3 * np.abs(lq))) + 1e-37
-            tol[at] = tau * abs(gr) * total * q[at] * R(V) + 4 * U * np.abs(wgrad[at]) + 1e-37
-            if dtype == torch.bfloat16:
-                tol = tol + 2.0 ** -8 * (np.abs(wgrad) + tol)
             assert abs(np.sum(out[r])) <= np.sum(tol), (r, np.sum(out[r]), np.sum(tol))
         near(out[r], wgrad, tol, (r, "gradient"))
 
