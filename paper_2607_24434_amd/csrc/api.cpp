@@ -1397,6 +1397,9 @@ namespace {
 static_assert(DE_TOP_MAX == de::kTopMax && DE_SCORE_STATS == de::kStats && DE_DISTILL_STATE == de::kState,
               "the header's sizes are the kernels'");
 
+// A launch has less than 2^32 threads; no memory holds logits for more.
+bool scores_too_many(int rows, int V) { return (int64_t)rows * ((V + 4095) / 4096) >= (1 << 24); }
+
 // The scratch of a vocabulary call: what its launches exchange, then the rows' statistics
 // or state where the caller keeps none.
 size_t scores_state_at(int rows, int V, int m) { return up256(de::scores_bytes(rows, V, m)); }
@@ -1409,8 +1412,7 @@ int vocab_rows(int rows, int V, int dtype, const void* logits, int ld, float tau
   if (!(tau >= 1e-30f && tau <= 1e30f)) return DE_ERR_INVALID;
   const uintptr_t mask = dtype == DE_BF16 ? 1 : 3;
   if (!logits || (reinterpret_cast<uintptr_t>(logits) & mask) != 0) return DE_ERR_INVALID;
-  // A launch has less than 2^32 threads; no memory holds logits for more.
-  if ((int64_t)rows * ((V + 4095) / 4096) >= (1 << 24)) return DE_ERR_UNSUPPORTED;
+  if (scores_too_many(rows, V)) return DE_ERR_UNSUPPORTED;
   x->rows = rows;
   x->V = V;
   x->bf16 = dtype == DE_BF16;
@@ -1451,6 +1453,7 @@ int check_scores_ws(int rows, int V, int m, const void* ws, size_t ws_bytes) {
 
 size_t de_scores_workspace_bytes(int rows, int V, int m) {
   if (rows < 1 || rows > (1 << 20) || V < 1 || V > (1 << 30) || m < 0 || m > DE_TOP_MAX) return 0;
+  if (scores_too_many(rows, V)) return 0;
   return scores_state_at(rows, V, m) + up256((size_t)rows * (DE_TOP_MAX + DE_DISTILL_STATE) * 4);
 }
 
