@@ -237,8 +237,12 @@ def _ptr(t):
 def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    # The handle alone: torch.cuda.current_stream() makes an object of it in 2.7 us.
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    # The handle alone, where torch has it (a private name): torch.cuda.current_stream() makes
+    # an object of it in 2.7 us.
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
 
 
 def _check(fn: str, rc: int):
