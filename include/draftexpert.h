@@ -679,7 +679,9 @@ int de_token_scores_grad(int rows, int V, int dtype, const void* logits, int ld,
  *     dlogits_v = g tau (W q_v - p_v) for entries, g tau q_v (W - P / Q) for the other
  *     tokens, W = sum_S p_j + P (1 and P = 0 with tail = 0).  W is 1 unless sum_S p_j is
  *     more (log probabilities stored in few bits may sum to that), or the last term is
- *     left out, and P with it (then sum_S p_j).  A row's gradient sums to zero. */
+ *     left out, and P with it (then sum_S p_j).  A row's gradient sums to zero.
+ * With tail = 1 the loss is a small difference of terms weighted by tau^2: from a tau of about
+ * 1e4 on, the values' own rounding shows in it. */
 int de_topk_distill(int rows, int V, int dtype, const void* logits, int ld, int m,
                     const int32_t* ids, const float* values, int tail, float tau, float* loss,
                     float* state, const de_row_grad* grad, void* ws, size_t ws_bytes,

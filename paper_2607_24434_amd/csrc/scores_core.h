@@ -216,7 +216,9 @@ __device__ __forceinline__ void each_slot(Tile<NTH, U>& x, const F& f) {
   if (x.ragged) f(x.last, x.m);
 }
 
-// Writes a slot of results to the row `out`, whose slots are those of w (same offset) or not.
+// Writes a slot of results to the row `out`, whose slots are those of w (same offset) or not: then
+// by the element, at twice the time (us, gradients of 2048 bf16 rows of 65537 in padded logits,
+// padded alike and packed: token scores 106 and 213, distillation 113 and 227).
 template <typename T>
 __device__ __forceinline__ void store_slot(const Row& w, const Row& out, int s, const float (&v)[kE<T>]) {
   if (out.o == w.o && s >= w.f0 && s < w.f1) {
@@ -528,7 +530,8 @@ inline Split split_of(const VocabRows& x, int m, void* ws) {
 
 // Whole rows in one block's registers, which then write the gradient too: logits are read
 // once and gradients written once.  Threads and slots a thread; at most 512 threads of 256
-// registers, 50 slots of them the row's (102400 fp32 logits).
+// registers, of which the distillation takes 250 with 50 slots (102400 fp32 logits; 52 spill).
+// Token scores take 224 to 229 there and keep the same limit.
 template <int NTH, int U>
 struct Whole {
   static constexpr int kNth = NTH, kU = U;
@@ -567,7 +570,9 @@ constexpr int whole_waves(int nth, int u) { return u < 50 ? 4 : nth / 256; }
 // grain does.  us, loss and gradient, whole and parts: 1 row of 50000 fp32 16
 // and 17, 64 rows of 60000 bf16 17 and 17, of 102400 fp32 27 and 25, bf16 26 and 21, 128
 // rows 28 and 37, 27 and 28, 256 rows 40 and 65, 30 and 39.
-// Without a gradient, 64 rows of 50000 fp32 9.4 and 12, 256 12 and 12, 333 17 and 15.
+// Without a gradient, 64 rows of 50000 fp32 9.4 and 12, 256 12 and 12, 333 17 and 15: two blocks
+// of 512 threads a CU.  Rows of other blocks (four of 256 threads a CU) take the same limit,
+// where the crossing was not measured.
 template <typename T>
 inline bool whole_pays(const VocabRows& x, bool grad) {
   const int slots = slots_most<T>(x);
